@@ -239,7 +239,7 @@ def _turned(x, weight, cos, sin, c):
 
 def _dense(packed, s):
     rows, idx, val = packed
-    x = rows.float()
+    x = rows.to(torch.float32, copy=True)  # (float32 rows would be added to where they lie)
     flat = x.view(len(rows), -1)
     flat[s["residual"].unsqueeze(1), idx] += val
     return x * s["scale"][:, None, None]
