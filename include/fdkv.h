@@ -227,6 +227,71 @@ fdkv_status fdkv_decode_attn_host(fdkv_ctx* ctx, int32_t layer, int32_t batch, c
 fdkv_status fdkv_decode_step_host(fdkv_ctx* ctx, int32_t batch, const void* q /*HOST*/, const void* k_new /*HOST*/,
                                   const void* v_new /*HOST*/, void* out /*HOST*/, int32_t out_dtype, void* stream);
 
+/*
+ * Decode attention of a batch whose sequences continue ONE committed prompt (samples of a prompt, users of one system prompt),
+ * whose compressed rows are read and reconstructed once for the whole batch instead of once per sequence.
+ * Row b of q, k_new, v_new and out belongs to sequence slot seqs[b]:
+ *   out = softmax over (rows 0..T-1 of the prompt in slot `prompt_seq`, as fdkv_decode_attn reconstructs them, then the layer's
+ *   tail rows of slot seqs[b]) of khat . q / sqrt(d), times vhat.
+ * Layouts, the append of k_new / v_new (to the tails of the slots seqs[b]), stream order and CUDA graphs: as fdkv_decode_attn.
+ * seqs: HOST int32[batch], distinct slots, batch <= 1024; each is prompt_seq itself (which then goes on with its own tail) or a
+ * slot without a committed prompt (FDKV_ERR_STATE).  A sequence may have no tail rows at all.  The prompt is what the slot holds
+ * committed at the time of the call: after fdkv_fold_tail on it, the folded tokens belong to it for every sequence.
+ * bf16 storage with head_dim 128: the probabilities are rounded to bf16 for the second product (float32 sums), so that out is
+ * within about 2e-3 of the exact attention; float32 storage: 1e-6.  FDKV_ROWS_E4M3 contexts: FDKV_ERR_UNSUPPORTED.
+ */
+fdkv_status fdkv_decode_attn_shared(fdkv_ctx* ctx, int32_t layer, int32_t prompt_seq, const int32_t* seqs /*HOST*/, int32_t batch, const void* q,
+                                    const void* k_new, const void* v_new, void* out, int32_t out_dtype, void* stream);
+
+/* Appends n rows to one layer's tail of a sequence slot, committed or not (a sequence's own tokens behind a shared prompt): element
+ * (t, h, ch) of k / v at ptr + t * stride_t + h * stride_h + ch, t < n, as in fdkv_compress_prefill.  FDKV_ERR_STATE where the tail
+ * has no room for them.  n = 0 does nothing.  May not be captured into a graph that is replayed (the length is the host's).     */
+fdkv_status fdkv_append_tail(fdkv_ctx* ctx, int32_t layer, int32_t seq, int32_t n, const void* k, const void* v, int64_t stride_t, int64_t stride_h,
+                             void* stream);
+
+/*
+ * What a layer does to the rows of its projection before the calls above take them: the RMS norm of every head's query and key
+ * and the rotation of their channels by the token's position, in one pass.
+ *   y = x / sqrt(mean_c x_c^2 + eps) * w                      over the head's channels (weights NULL: y = x)
+ *   (a, b) -> (a cos - b sin, b cos + a sin) * scale          for the channel pair of frequency i < rotary_dim / 2:
+ *        channels (i, i + rotary_dim / 2), or (2 i, 2 i + 1) when `interleaved`; the angle is
+ *        positions[axis_of[i]][t] * inv_freq[i] in float64.   Channels from rotary_dim on are only normed.
+ * float32 arithmetic, one rounding to the storage type at the end.  Several axes: time, height and width of images and video.
+ */
+typedef struct {
+    int32_t n_q_heads;      /* 1 .. 1024 */
+    int32_t n_kv_heads;     /* 1 .. 1024 */
+    int32_t head_dim;       /* 64 or 128 */
+    int32_t dtype;          /* fdkv_dtype of the rows and the weights */
+    int32_t rotary_dim;     /* a multiple of 16, 0 .. head_dim (0: no rotation) */
+    int32_t interleaved;
+    int32_t n_axes;         /* position axes, 1 .. 4 */
+    float eps;              /* finite, >= 0 */
+    float scale;            /* factor of cos and sin (1 for a plain rotation) */
+    const float* inv_freq;  /* HOST [rotary_dim / 2], finite; may be NULL when rotary_dim is 0 */
+    const int32_t* axis_of; /* HOST [rotary_dim / 2], each in [0, n_axes); NULL: axis 0 for all */
+    const void* q_weight;   /* DEVICE [head_dim], 16-byte aligned; NULL: queries are not normed */
+    const void* k_weight;   /* likewise for the keys */
+} fdkv_rotary;
+
+/* n tokens.  Element (t, h, ch) of a tensor at ptr + t * stride_t + h * stride_h + ch; pointers 16-byte aligned, strides in elements,
+ * multiples of 8 and at least head_dim.  q and q_out (or k and k_out) may both be NULL: that side is left out.  An output may be
+ * its own input (same pointer and strides); no other overlap.  positions: DEVICE int32 [n_axes][n], axes pos_stride elements apart (not read
+ * and may be NULL when rotary_dim is 0).  n = 0 does nothing.  The HOST arrays of `r` are read during the call.             */
+fdkv_status fdkv_qk_norm_rope(const fdkv_rotary* r /*HOST*/, int64_t n, const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k,
+                              int64_t k_stride_t, int64_t k_stride_h, const int32_t* positions, int64_t pos_stride, void* q_out,
+                              int64_t qo_stride_t, int64_t qo_stride_h, void* k_out, int64_t ko_stride_t, int64_t ko_stride_h, void* stream);
+
+/*
+ * A decode step of one layer from the rows of its fused projection: fdkv_qk_norm_rope, then fdkv_decode_attn (prompt_seq = -1, seqs
+ * NULL: slots 0 .. batch-1, each on its own prompt) or fdkv_decode_attn_shared (prompt_seq >= 0), which appends the new rows.
+ * qkv: [batch] rows, `stride` elements apart (a multiple of 8, >= (n_q_heads + 2 n_kv_heads) * head_dim), each the query heads, the key heads and the value
+ * heads one after the other.  positions: DEVICE int32 [n_axes][batch], dense.  r's heads, head_dim and dtype are the context's.
+ * Between the steps the rows lie in the context's workspace (the staging of the *_host calls).
+ */
+fdkv_status fdkv_decode_qkv(fdkv_ctx* ctx, int32_t layer, int32_t prompt_seq, const int32_t* seqs /*HOST*/, int32_t batch, const fdkv_rotary* r /*HOST*/,
+                            const void* qkv, int64_t stride, const int32_t* positions, void* out, int32_t out_dtype, void* stream);
+
 /* Sets the tail length of every layer of a sequence (0 empties the tails; n <= current length). */
 fdkv_status fdkv_set_tail_len(fdkv_ctx* ctx, int32_t seq, int32_t n, void* stream);
 
@@ -335,7 +400,9 @@ typedef enum {
     FDKV_KERNEL_DECODE_FAST = 2,    /* decode_fast_kernel: TMA + tensor-core decode attention */
     FDKV_KERNEL_DECODE_PORTABLE = 3,/* decode_generic_kernel + combine_kernel                */
     FDKV_KERNEL_TOKEN_SCORE = 4,    /* token_score_kernel: tcgen05 token scores              */
-    FDKV_KERNEL_COUNT_ = 5
+    FDKV_KERNEL_SHARED_TC = 5,      /* shared_tc_kernel: tcgen05 attention of a batch on one prompt */
+    FDKV_KERNEL_SHARED_PORTABLE = 6,/* shared_part_kernel: the same in float32 FMA */
+    FDKV_KERNEL_COUNT_ = 7
 } fdkv_kernel_id;
 int64_t fdkv_kernel_launch_count(int32_t kernel);
 

@@ -34,6 +34,11 @@ class _Config(C.Structure):
                                          "max_tail", "dtype", "keep_num", "keep_den", "residual_rule", "block_size", "max_fold", "row_format")]
 
 
+class _Rotary(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "dtype", "rotary_dim", "interleaved", "n_axes")] + \
+               [("eps", C.c_float), ("scale", C.c_float)] + [(n, C.c_void_p) for n in ("inv_freq", "axis_of", "q_weight", "k_weight")]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2607_06519_b200.build` "
@@ -53,6 +58,10 @@ def _load():
         "fdkv_decode_attn": [vp, i32, i32, vp, vp, vp, vp, i32, vp],
         "fdkv_decode_attn_host": [vp, i32, i32, vp, vp, vp, vp, i32, vp],
         "fdkv_decode_step_host": [vp, i32, vp, vp, vp, vp, i32, vp],
+        "fdkv_decode_attn_shared": [vp, i32, i32, vp, i32, vp, vp, vp, vp, i32, vp],
+        "fdkv_append_tail": [vp, i32, i32, i32, vp, vp, i64, i64, vp],
+        "fdkv_qk_norm_rope": [P(_Rotary), i64, vp, i64, i64, vp, i64, i64, vp, i64, vp, i64, i64, vp, i64, i64, vp],
+        "fdkv_decode_qkv": [vp, i32, i32, vp, i32, P(_Rotary), vp, i64, vp, vp, i32, vp],
         "fdkv_set_tail_len": [vp, i32, i32, vp],
         "fdkv_fold_tail": [vp, i32, i32, vp],
         "fdkv_get_rows_e4m3": [vp, i32, i32, i32, i32, vp, vp, vp],
@@ -85,13 +94,15 @@ def _load():
 
 _lib = _load()
 _decode_attn = _lib.fdkv_decode_attn
+_decode_attn_shared = _lib.fdkv_decode_attn_shared
+_qk_norm_rope = _lib.fdkv_qk_norm_rope
 
 
 def launch_count() -> int:
     return int(_lib.fdkv_launch_count())
 
 
-KERNEL_PROBE_TC, KERNEL_PROBE_PORTABLE, KERNEL_DECODE_FAST, KERNEL_DECODE_PORTABLE, KERNEL_TOKEN_SCORE = range(5)
+KERNEL_PROBE_TC, KERNEL_PROBE_PORTABLE, KERNEL_DECODE_FAST, KERNEL_DECODE_PORTABLE, KERNEL_TOKEN_SCORE, KERNEL_SHARED_TC, KERNEL_SHARED_PORTABLE = range(7)
 
 
 def kernel_launch_count(kernel: int) -> int:
@@ -179,6 +190,85 @@ def compress_unit_noalloc(x0, x1, keep_num: int, keep_den: int, z0_out, idx_out,
                                            _ptr(idx_out), _ptr(val_out), C.byref(cnt), _stream(stream)),
            "fdkv_compress_unit_noalloc")
     return int(cnt.value)
+
+
+class Rotary:
+    """What fdkv_qk_norm_rope does to a layer's queries and keys (fdkv_rotary): kept by the caller beside the layer's weights.
+
+    inv_freq: one frequency per rotating pair of channels; axis_of: the position axis that turns it (None: axis 0 for all);
+    q_weight / k_weight: RMS norm weights [head_dim] on the device (None: no norm).
+    """
+
+    def __init__(self, inv_freq, axis_of=None, n_axes=1, interleaved=False, q_weight=None, k_weight=None, eps=1e-6, scale=1.0):
+        m = len(inv_freq)
+        if axis_of is not None and len(axis_of) != m:
+            raise ValueError("axis_of needs one entry per frequency")
+        for w in (q_weight, k_weight):
+            if w is not None and (w.dim() != 1 or w.stride(0) != 1):
+                raise ValueError("norm weights must be dense [head_dim] tensors")
+        self._inv = (C.c_float * max(m, 1))(*[float(f) for f in inv_freq])
+        self._axis = None if axis_of is None else (C.c_int32 * max(m, 1))(*[int(a) for a in axis_of])
+        self.n_axes, self.q_weight, self.k_weight = n_axes, q_weight, k_weight
+        self._c = _Rotary(1, 1, 0, 0, 2 * m, int(interleaved), n_axes, eps, scale, C.addressof(self._inv),
+                          None if self._axis is None else C.addressof(self._axis),
+                          None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
+
+    def c(self, n_q_heads: int, n_kv_heads: int, head_dim: int, tdtype) -> _Rotary:
+        for w in (self.q_weight, self.k_weight):
+            if w is not None and (w.dtype is not tdtype or len(w) != head_dim):
+                raise ValueError("norm weights must have the rows' dtype and head_dim")
+        r = self._c
+        r.n_q_heads, r.n_kv_heads, r.head_dim, r.dtype = n_q_heads, n_kv_heads, head_dim, _dtype_code(tdtype)
+        return r
+
+
+def _dtype_code(tdtype) -> int:
+    if tdtype is torch.bfloat16:
+        return BF16
+    if tdtype is torch.float32:
+        return F32
+    raise ValueError("rows must be bfloat16 or float32")
+
+
+def _positions(positions, n_axes: int, n: int) -> int:
+    """The distance between the axes of positions [n_axes, n], or [n] for one axis."""
+    if positions.dtype is not torch.int32 or tuple(positions.shape) not in ((n_axes, n),) + (((n,),) if n_axes == 1 else ()) or (n > 1 and positions.stride(-1) != 1):
+        raise ValueError("positions must be int32 [n_axes, n], dense along n")
+    return positions.stride(0) if positions.dim() == 2 and n_axes > 1 else n
+
+
+def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream=None):
+    """Norm and rotation of queries [n, n_q_heads, d] and keys [n, n_kv_heads, d] (either may be None); returns (q_out, k_out).
+    Tensors may be strided (a slice of the fused projection, a layer's rows); an output may be its own input."""
+    x = q if q is not None else k
+    n, _, d = x.shape
+    if q_out is None and q is not None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None and k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    args = []
+    for t, like in ((q, q), (k, k), (q_out, q), (k_out, k)):
+        if t is None:
+            args.append((None, 0, 0))
+            continue
+        st, sh, sc = t.stride()
+        if sc != 1 or t.dtype is not x.dtype or t.shape != like.shape or t.shape[0] != n or t.shape[2] != d:
+            raise ValueError("queries and keys must be [n, heads, d] of one dtype, dense along d")
+        args.append((t.data_ptr(), st if n > 1 else d, sh if t.shape[1] > 1 else d))
+    step = _positions(positions, rotary.n_axes, n) if positions is not None else 0
+    c = rotary.c(q.shape[1] if q is not None else 1, k.shape[1] if k is not None else 1, d, x.dtype)
+    st = _qk_norm_rope(c, n, *args[0], *args[1], None if positions is None else positions.data_ptr(), step, *args[2], *args[3], _stream(stream))
+    if st:
+        raise FdkvError(st, "fdkv_qk_norm_rope")
+    return q_out, k_out
+
+
+def _slots(seqs):
+    """Sequence slots as a HOST int32 array: (address, count, what keeps it alive).  An int32 CPU tensor is passed as it is."""
+    if isinstance(seqs, torch.Tensor) and seqs.dtype is torch.int32 and seqs.device.type == "cpu" and seqs.is_contiguous():
+        return seqs.data_ptr(), seqs.numel(), seqs
+    arr = (C.c_int32 * max(len(seqs), 1))(*[int(x) for x in seqs])
+    return C.addressof(arr), len(seqs), arr
 
 
 class Context:
@@ -276,6 +366,49 @@ class Context:
         if st:
             raise FdkvError(st, "fdkv_decode_attn")
         return out
+
+    def decode_attn_shared(self, layer, prompt_seq, seqs, q, k_new=None, v_new=None, out=None, out_dtype=None, stream=None):
+        """Decode attention of sequences that continue the prompt of slot `prompt_seq`: q [len(seqs), n_q_heads, d], row b for slot
+        seqs[b]; returns out [len(seqs), n_q_heads, d]."""
+        od = self.cfg.dtype if out_dtype is None else out_dtype
+        slots, n, _keep = _slots(seqs)
+        if len(q) != n:
+            raise ValueError("q needs one row per sequence")
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16 if od == BF16 else torch.float32, device=self.device)
+        st = _decode_attn_shared(self.h, layer, prompt_seq, slots, n, q.data_ptr(), None if k_new is None else k_new.data_ptr(),
+                                 None if v_new is None else v_new.data_ptr(), out.data_ptr(), od, _stream(stream))
+        if st:
+            raise FdkvError(st, "fdkv_decode_attn_shared")
+        return out
+
+    def decode_qkv(self, layer, rotary: Rotary, qkv, positions, prompt_seq=-1, seqs=None, out=None, out_dtype=None, stream=None):
+        """A decode step of one layer from its fused projection rows [batch, (n_q_heads + 2 n_kv_heads) * d]: norm, rotation, append
+        and attention, each sequence on its own prompt, or (prompt_seq, seqs) all on one."""
+        od = self.cfg.dtype if out_dtype is None else out_dtype
+        c = self.cfg
+        n = len(qkv)
+        if qkv.dim() != 2 or qkv.dtype is not self.tdtype or qkv.shape[1] != (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim or qkv.stride(1) != 1:
+            raise ValueError("qkv must be [batch, (n_q_heads + 2 n_kv_heads) * head_dim] of the context dtype")
+        if positions is not None and _positions(positions, rotary.n_axes, n) != n:
+            raise ValueError("positions must be dense")
+        slots, ns, _keep = (None, n, None) if seqs is None else _slots(seqs)
+        if ns != n:
+            raise ValueError("qkv needs one row per sequence")
+        if out is None:
+            out = torch.empty((n, c.n_q_heads, c.head_dim), dtype=torch.bfloat16 if od == BF16 else torch.float32, device=self.device)
+        _check(_lib.fdkv_decode_qkv(self.h, layer, prompt_seq, slots, n, rotary.c(c.n_q_heads, c.n_kv_heads, c.head_dim, self.tdtype), qkv.data_ptr(),
+                                    qkv.stride(0) if n > 1 else qkv.shape[1], _ptr(positions), out.data_ptr(), od, _stream(stream)), "fdkv_decode_qkv")
+        return out
+
+    def append_tail(self, layer, seq, k, v, stream=None):
+        """Appends rows k, v [n, n_kv_heads, d] (one strided layout) to a layer's tail of a sequence slot."""
+        if k.shape != v.shape or k.stride() != v.stride() or k.dtype is not self.tdtype or v.dtype is not self.tdtype or k.stride(2) != 1 or \
+                tuple(k.shape[1:]) != (self.cfg.n_kv_heads, self.cfg.head_dim):
+            raise ValueError("k and v must share one [n, Hkv, d] strided layout and the context dtype")
+        n, d = len(k), self.cfg.head_dim
+        _check(_lib.fdkv_append_tail(self.h, layer, seq, n, _ptr(k), _ptr(v), k.stride(0) if n > 1 else d, k.stride(1) if k.shape[1] > 1 else d, _stream(stream)),
+               "fdkv_append_tail")
 
     def decode_attn_host(self, layer, q, k_new, v_new, out, out_dtype, stream=None):
         """Same with host (ideally pinned) tensors; synchronous."""

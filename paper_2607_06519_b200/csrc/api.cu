@@ -801,19 +801,22 @@ fdkv_status fdkv_commit(fdkv_ctx* c, int32_t seq, void* stream) {
     return FDKV_OK;
 }
 
+// Every sequence committed and, where a row is appended, with room in its tail.
+static fdkv_status decode_ready(fdkv_ctx* c, int32_t layer, int32_t batch, bool append) {
+    for (int b = 0; b < batch; ++b)
+        if (!c->seqs[b].committed || (append && c->seqs[b].tail_len[layer] >= c->s.max_tail)) return FDKV_ERR_STATE;
+    return FDKV_OK;
+}
+
 static fdkv_status decode_impl(fdkv_ctx* c, int32_t layer, int32_t batch, const void* q, const void* k_new,
                                const void* v_new, void* out, int32_t out_dtype, cudaStream_t st) {
     const Shape& s = c->s;
+    const fdkv_status ready = decode_ready(c, layer, batch, k_new != nullptr);
+    if (ready != FDKV_OK) return ready;
     int Tmax = 0;
-    for (int b = 0; b < batch; ++b) {
-        if (!c->seqs[b].committed) return FDKV_ERR_STATE;
-        Tmax = c->seqs[b].T > Tmax ? c->seqs[b].T : Tmax;
-    }
-    if (k_new) {
-        for (int b = 0; b < batch; ++b)
-            if (c->seqs[b].tail_len[layer] >= s.max_tail) return FDKV_ERR_STATE;
+    for (int b = 0; b < batch; ++b) Tmax = c->seqs[b].T > Tmax ? c->seqs[b].T : Tmax;
+    if (k_new)
         for (int b = 0; b < batch; ++b) c->seqs[b].tail_len[layer]++;
-    }
     std::vector<int32_t>&host_T = c->host_T, &host_modes = c->host_modes, &host_tail = c->host_tail;
     host_T.resize(batch); host_modes.resize((size_t)batch * s.Hkv); host_tail.resize(batch);
     for (int b = 0; b < batch; ++b) {
@@ -906,6 +909,161 @@ fdkv_status fdkv_decode_step_host(fdkv_ctx* c, int32_t batch, const void* q, con
     CU(cudaMemcpyAsync(out, c->work + c->ws.io_out, ob * s.L, cudaMemcpyDeviceToHost, st));
     CU(cudaStreamSynchronize(st));
     return FDKV_OK;
+}
+
+// What fdkv_decode_attn_shared asks of its sequences; `append`: a row joins every tail.
+static fdkv_status shared_ready(fdkv_ctx* c, int32_t layer, int32_t prompt, const int32_t* seqs, int32_t batch, bool append) {
+    const Shape& s = c->s;
+    if (!seqs || prompt < 0 || prompt >= s.max_batch || batch < 1 || batch > s.max_batch || batch > kMaxShared) return FDKV_ERR_INVALID_ARG;
+    std::vector<uint8_t>& seen = c->seen;
+    seen.assign(s.max_batch, 0);
+    for (int b = 0; b < batch; ++b) {
+        if (seqs[b] < 0 || seqs[b] >= s.max_batch || seen[seqs[b]]) return FDKV_ERR_INVALID_ARG;
+        seen[seqs[b]] = 1;
+    }
+    if (s.rows_f8) return FDKV_ERR_UNSUPPORTED;
+    if (!c->seqs[prompt].committed) return FDKV_ERR_STATE;
+    for (int b = 0; b < batch; ++b) {
+        if (seqs[b] != prompt && c->seqs[seqs[b]].committed) return FDKV_ERR_STATE;
+        if (append && c->seqs[seqs[b]].tail_len[layer] >= s.max_tail) return FDKV_ERR_STATE;
+    }
+    return FDKV_OK;
+}
+
+static fdkv_status shared_impl(fdkv_ctx* c, int32_t layer, int32_t prompt, const int32_t* seqs, int32_t batch, const void* q, const void* k_new, const void* v_new,
+                               void* out, int32_t out_dtype, cudaStream_t st) {
+    const Shape& s = c->s;
+    const fdkv_status ready = shared_ready(c, layer, prompt, seqs, batch, k_new != nullptr);
+    if (ready != FDKV_OK) return ready;
+    c->host_tail.resize(batch);
+    for (int b = 0; b < batch; ++b) c->host_tail[b] = c->seqs[seqs[b]].tail_len[layer] + (k_new ? 1 : 0);
+    SharedArgs a;
+    a.desc = arp<UnitDesc>(c, c->ar.desc) + ((size_t)prompt * s.L + layer) * s.Hkv;
+    a.batch = batch; a.Hq = s.Hq; a.Hkv = s.Hkv; a.G = s.G; a.d = s.d; a.T = c->seqs[prompt].T;
+    a.q = q; a.k_new = k_new; a.v_new = v_new; a.out = out; a.out_dtype = out_dtype;
+    const size_t tails = (size_t)layer * s.max_batch * s.Hkv * s.tail_rows * s.d * s.esize;
+    a.tail_k = c->arena + c->ar.tail_k + tails; a.tail_v = c->arena + c->ar.tail_v + tails;
+    a.tail_rows = s.tail_rows;
+    a.tail_len = arp<int32_t>(c, c->ar.tail_len) + (size_t)layer * s.max_batch;
+    a.seqs = seqs; a.lens = c->host_tail.data();
+    a.modes = c->seqs[prompt].modes.data() + (layer / s.B) * s.Hkv;
+    a.tmap = c->has_tmap ? c->tmap : nullptr;
+    a.arena_base = c->arena;
+    a.twice = c->packed_lists && s.B == 4;
+    a.partials = wsp<float>(c, c->ws.partials);
+    a.partial_floats = (int64_t)s.max_batch * s.Hq * kMaxSplits * (s.d + 4);
+    a.status = wsp<int32_t>(c, c->ws.status);
+    CU(launch_shared_decode(a, s.dtype, st));
+    if (k_new)
+        for (int b = 0; b < batch; ++b) c->seqs[seqs[b]].tail_len[layer]++;
+    return FDKV_OK;
+}
+
+fdkv_status fdkv_decode_attn_shared(fdkv_ctx* c, int32_t layer, int32_t prompt_seq, const int32_t* seqs, int32_t batch, const void* q, const void* k_new,
+                                    const void* v_new, void* out, int32_t out_dtype, void* stream) {
+    if (!c || !q || !out) return FDKV_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= c->s.L || (k_new == nullptr) != (v_new == nullptr)) return FDKV_ERR_INVALID_ARG;
+    if (out_dtype != FDKV_F32 && out_dtype != FDKV_BF16) return FDKV_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(k_new, 16) || !aligned(v_new, 16)) return FDKV_ERR_INVALID_ARG;
+    return shared_impl(c, layer, prompt_seq, seqs, batch, q, k_new, v_new, out, out_dtype, S(stream));
+}
+
+fdkv_status fdkv_append_tail(fdkv_ctx* c, int32_t layer, int32_t seq, int32_t n, const void* k, const void* v, int64_t stride_t, int64_t stride_h, void* stream) {
+    if (!seq_ok(c, seq) || layer < 0 || layer >= c->s.L || n < 0) return FDKV_ERR_INVALID_ARG;
+    if (n == 0) return FDKV_OK;
+    const Shape& s = c->s;
+    if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return FDKV_ERR_INVALID_ARG;
+    if (stride_h < s.d || stride_t < s.d || (stride_t % 8) || (stride_h % 8)) return FDKV_ERR_INVALID_ARG;
+    int32_t& len = c->seqs[seq].tail_len[layer];
+    if (n > s.max_tail - len) return FDKV_ERR_STATE;
+    const size_t row = (size_t)s.d * s.esize, head = (size_t)s.tail_rows * row;
+    const size_t at = ((size_t)layer * s.max_batch + seq) * s.Hkv * head + (size_t)len * row;
+    CU(launch_append_tail(k, v, stride_t * s.esize, stride_h * s.esize, c->arena + c->ar.tail_k + at, c->arena + c->ar.tail_v + at, (int64_t)head, n, s.Hkv, (int)row,
+                          arp<int32_t>(c, c->ar.tail_len) + (size_t)layer * s.max_batch + seq, len + n, S(stream)));
+    len += n;
+    return FDKV_OK;
+}
+
+// Checks `r` and fills in what a launch takes from it.
+static fdkv_status rotary_args(const fdkv_rotary& r, QkPrepArgs& a) {
+    if (r.n_q_heads < 1 || r.n_q_heads > 1024 || r.n_kv_heads < 1 || r.n_kv_heads > 1024) return FDKV_ERR_INVALID_ARG;
+    if (r.dtype != FDKV_F32 && r.dtype != FDKV_BF16) return FDKV_ERR_UNSUPPORTED;
+    if (r.head_dim != 64 && r.head_dim != 128) return FDKV_ERR_UNSUPPORTED;
+    if (r.rotary_dim < 0 || r.rotary_dim > r.head_dim) return FDKV_ERR_INVALID_ARG;
+    if (r.rotary_dim % 16) return FDKV_ERR_UNSUPPORTED;
+    if (r.n_axes < 1 || r.n_axes > 4 || !std::isfinite(r.eps) || r.eps < 0.f || !std::isfinite(r.scale)) return FDKV_ERR_INVALID_ARG;
+    if (r.rotary_dim && !r.inv_freq) return FDKV_ERR_INVALID_ARG;
+    if (!aligned(r.q_weight, 16) || !aligned(r.k_weight, 16)) return FDKV_ERR_INVALID_ARG;
+    for (int i = 0; i < r.rotary_dim / 2; ++i) {
+        const int axis = r.axis_of ? r.axis_of[i] : 0;
+        if (!std::isfinite(r.inv_freq[i]) || axis < 0 || axis >= r.n_axes) return FDKV_ERR_INVALID_ARG;
+        a.inv_freq[i] = r.inv_freq[i];
+        a.axis[i] = (uint8_t)axis;
+    }
+    a.rotary_dim = r.rotary_dim;
+    a.interleaved = r.interleaved != 0;
+    a.eps = r.eps;
+    a.scale = r.scale;
+    a.q_weight = r.q_weight;
+    a.k_weight = r.k_weight;
+    a.Hv = 0;
+    a.v = a.v_out = nullptr;
+    a.v_n = a.v_h = a.vo_n = a.vo_h = 0;
+    return FDKV_OK;
+}
+
+fdkv_status fdkv_qk_norm_rope(const fdkv_rotary* r, int64_t n, const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k, int64_t k_stride_t, int64_t k_stride_h,
+                              const int32_t* positions, int64_t pos_stride, void* q_out, int64_t qo_stride_t, int64_t qo_stride_h, void* k_out, int64_t ko_stride_t,
+                              int64_t ko_stride_h, void* stream) {
+    QkPrepArgs a;
+    if (!r || n < 0 || n >= (int64_t)1 << 31) return FDKV_ERR_INVALID_ARG;
+    const fdkv_status st = rotary_args(*r, a);
+    if (st != FDKV_OK) return st;
+    if (!q != !q_out || !k != !k_out) return FDKV_ERR_INVALID_ARG;
+    if (n == 0) return FDKV_OK;
+    if ((!q && !k) || (r->rotary_dim && !positions) || (reinterpret_cast<uintptr_t>(positions) % 4) || (r->n_axes > 1 && pos_stride < n)) return FDKV_ERR_INVALID_ARG;
+    auto strides_ok = [&](const void* p, int64_t t, int64_t h) { return !p || (aligned(p, 16) && t >= r->head_dim && h >= r->head_dim && t % 8 == 0 && h % 8 == 0); };
+    if (!strides_ok(q, q_stride_t, q_stride_h) || !strides_ok(k, k_stride_t, k_stride_h) || !strides_ok(q_out, qo_stride_t, qo_stride_h) ||
+        !strides_ok(k_out, ko_stride_t, ko_stride_h))
+        return FDKV_ERR_INVALID_ARG;
+    a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out;
+    a.q_n = q_stride_t; a.q_h = q_stride_h; a.k_n = k_stride_t; a.k_h = k_stride_h;
+    a.qo_n = qo_stride_t; a.qo_h = qo_stride_h; a.ko_n = ko_stride_t; a.ko_h = ko_stride_h;
+    a.n = n;
+    a.pos = positions; a.pos_stride = pos_stride;
+    a.Hq = q ? r->n_q_heads : 0;
+    a.Hk = k ? r->n_kv_heads : 0;
+    CU(launch_qk_prep(a, r->dtype, r->head_dim, S(stream)));
+    return FDKV_OK;
+}
+
+fdkv_status fdkv_decode_qkv(fdkv_ctx* c, int32_t layer, int32_t prompt_seq, const int32_t* seqs, int32_t batch, const fdkv_rotary* r, const void* qkv, int64_t stride,
+                            const int32_t* positions, void* out, int32_t out_dtype, void* stream) {
+    if (!c || !r || !qkv || !out) return FDKV_ERR_INVALID_ARG;
+    const Shape& s = c->s;
+    if (layer < 0 || layer >= s.L || batch < 1 || batch > s.max_batch || prompt_seq < -1 || (prompt_seq < 0 && seqs)) return FDKV_ERR_INVALID_ARG;
+    if (out_dtype != FDKV_F32 && out_dtype != FDKV_BF16) return FDKV_ERR_INVALID_ARG;
+    if (r->n_q_heads != s.Hq || r->n_kv_heads != s.Hkv || r->head_dim != s.d || r->dtype != s.dtype) return FDKV_ERR_INVALID_ARG;
+    QkPrepArgs a;
+    const fdkv_status st = rotary_args(*r, a);
+    if (st != FDKV_OK) return st;
+    if (stride < (int64_t)(s.Hq + 2 * s.Hkv) * s.d || stride % 8 || !aligned(qkv, 16) || !aligned(out, 16)) return FDKV_ERR_INVALID_ARG;
+    if ((r->rotary_dim && !positions) || (reinterpret_cast<uintptr_t>(positions) % 4)) return FDKV_ERR_INVALID_ARG;
+    const fdkv_status ready = prompt_seq < 0 ? decode_ready(c, layer, batch, true) : shared_ready(c, layer, prompt_seq, seqs, batch, true);
+    if (ready != FDKV_OK) return ready;
+    const char* const row = (const char*)qkv;
+    a.q = row; a.k = row + (size_t)s.Hq * s.d * s.esize; a.v = row + (size_t)(s.Hq + s.Hkv) * s.d * s.esize;
+    a.q_out = c->work + c->ws.io_q; a.k_out = c->work + c->ws.io_k; a.v_out = c->work + c->ws.io_v;
+    a.q_n = a.k_n = a.v_n = stride;
+    a.q_h = a.k_h = a.v_h = a.qo_h = a.ko_h = a.vo_h = s.d;
+    a.qo_n = (int64_t)s.Hq * s.d;
+    a.ko_n = a.vo_n = (int64_t)s.Hkv * s.d;
+    a.Hq = s.Hq; a.Hk = a.Hv = s.Hkv;
+    a.n = batch;
+    a.pos = positions; a.pos_stride = batch;
+    CU(launch_qk_prep(a, s.dtype, s.d, S(stream)));
+    if (prompt_seq < 0) return decode_impl(c, layer, batch, a.q_out, a.k_out, a.v_out, out, out_dtype, S(stream));
+    return shared_impl(c, layer, prompt_seq, seqs, batch, a.q_out, a.k_out, a.v_out, out, out_dtype, S(stream));
 }
 
 fdkv_status fdkv_set_tail_len(fdkv_ctx* c, int32_t seq, int32_t n, void* stream) {

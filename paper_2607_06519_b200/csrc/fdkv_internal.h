@@ -149,6 +149,7 @@ struct fdkv_ctx {
     std::vector<fdkv::UnitDesc> desc_host;  // [max_batch][L][Hkv]
     uint64_t plan_epoch = 1;                // advanced whenever a committed length or mode changes
     std::vector<fdkv::FastPlan> plans;      // [L]
+    std::vector<uint8_t> seen;              // [max_batch] slots that a call of a shared prompt has named
     std::vector<int32_t> host_T, host_modes, host_tail;  // what a decode call's launch is planned from (kept: no allocation per call)
     alignas(64) unsigned char tmap[128];    // CUtensorMap of the arena (bf16, head_dim 128 only)
     bool has_tmap = false;
@@ -374,6 +375,57 @@ struct TokenArgs {
 inline int token_err_slots(int B, int G, bool tensor_core, int W) { return tensor_core ? B * ((G * W + 255) / 256) : 1; }
 // tensor_core: bf16 / head_dim 128 contexts (tcgen05 score kernel); otherwise the float32 score kernel
 cudaError_t launch_token_select(const TokenArgs& a, int dtype, int d, bool tensor_core, cudaStream_t st);
+
+// ---- rows of a projection: norm and rotation (qk_prep.cu) ----
+struct QkPrepArgs {
+    const void *q, *k, *v;  // element (t, h, c) at t * _n + h * _h + c; v rows (Hv > 0) are copied as they are
+    void *q_out, *k_out, *v_out;
+    int64_t q_n, q_h, k_n, k_h, v_n, v_h, qo_n, qo_h, ko_n, ko_h, vo_n, vo_h;
+    int64_t n, pos_stride;
+    int Hq, Hk, Hv;
+    int rotary_dim, interleaved;
+    float eps, scale;
+    const void *q_weight, *k_weight;
+    const int32_t* pos;      // [axes], pos_stride apart, of [n]
+    float inv_freq[64];      // [rotary_dim / 2]
+    uint8_t axis[64];
+};
+cudaError_t launch_qk_prep(const QkPrepArgs& a, int dtype, int d, cudaStream_t st);
+// n rows per head behind a tail's rows (tail_k / tail_v: the first row to write of head 0), and the device's copy of the length.
+// Strides in bytes.
+cudaError_t launch_append_tail(const void* k, const void* v, int64_t stride_t, int64_t stride_h, void* tail_k, void* tail_v, int64_t head_bytes, int n, int H, int row_bytes,
+                               int32_t* len, int new_len, cudaStream_t st);
+
+// ---- decode attention of a batch on one committed prompt (shared_prefix.cu, shared_tc.cu) ----
+constexpr int kMaxShared = 1024;     // sequences of one call
+constexpr int kSharedFew = 64;       // ... whose lists travel as a short parameter
+constexpr int kSharedTile = 128;     // prompt tokens per tile
+// The prompt part's work: items (KV head, group of query rows), item-major, of `tiles` tiles each, cut into one range per block.
+// Block c works on tiles [start[c], start[c + 1]) of that list; its part of item u has number c + u.
+struct SharedSched {
+    int start[kMaxSplits + 1];
+    int ncta, tiles, groups, row_tile;  // blocks, tiles per item, row groups per KV head, query rows per group
+};
+struct SharedArgs {
+    const UnitDesc* desc;  // [Hkv] of the prompt and layer
+    int batch, Hq, Hkv, G, d, T;
+    const void *q, *k_new, *v_new;
+    void* out;
+    int out_dtype;
+    void *tail_k, *tail_v;  // the layer's tails: [max_batch][Hkv][tail_rows][d]
+    int tail_rows;
+    int32_t* tail_len;      // the layer's device copies of the lengths: [max_batch]
+    const int32_t *seqs, *lens;  // HOST [batch]: slots, and their tail lengths with this call's append
+    const int32_t* modes;   // HOST [Hkv]
+    const void* tmap;       // CUtensorMap over the arena as rows of 256 bytes (bf16, head_dim 128), or null
+    const void* arena_base;
+    int twice;              // packed lists: the deviations of a block of four are stored doubled
+    float* partials;        // a part: [d / 4][row_tile][4] accumulators, then [row_tile] maxima and [row_tile] sums
+    int64_t partial_floats;
+    int32_t* status;
+};
+inline __host__ __device__ int64_t shared_part_floats(int row_tile, int d) { return (int64_t)row_tile * (d + 4); }
+cudaError_t launch_shared_decode(const SharedArgs& a, int dtype, cudaStream_t st);
 
 // Function attributes (the opt-in to large dynamic shared memory) and the SM count belong to a device, not to the
 // process: every launcher keeps one of these and runs its set-up the first time it meets the current device.
