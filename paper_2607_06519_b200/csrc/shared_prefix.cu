@@ -114,14 +114,7 @@ __global__ void __launch_bounds__(kThreads) shared_part_kernel(SharedArgs a, con
                     float* const to = is_v ? sv : sk;
                     const int e0 = off[s0], e1 = off[s1];
                     if (ud.res_kind == 1) {  // whole rows of selected tokens
-                        for (int i = e0 * D + tid; i < e1 * D; i += kThreads) to[(idx[i / D] - tok) * P + i % D] += (a.twice ? (sign < 0.f ? -1.f : 1.f) : sign) * ldf<T>(val + i);
-                    } else if (!val) {  // packed words: value, and its place in the slice's swizzled tile
-                        const int mid = off[min(s0 + 1, s1)];
-                        for (int e = e0 + tid; e < e1; e += kThreads) {
-                            const uint32_t w = (uint32_t)idx[e], o = w >> 15 & ~1u, in = o & 2047, row = in >> 7;
-                            const uint32_t ch = (o >> 11) * 64 + ((in >> 4 & 7) ^ (row & 7)) * 8 + (in >> 1 & 7);
-                            to[(row + (e >= mid ? 16 : 0)) * P + ch] += (sign < 0.f ? -1.f : 1.f) * __uint_as_float(w << 16);
-                        }
+                        for (int i = e0 * D + tid; i < e1 * D; i += kThreads) to[(idx[i / D] - tok) * P + i % D] += sign * ldf<T>(val + i);
                     } else {
                         for (int e = e0 + tid; e < e1; e += kThreads) {
                             const int at = idx[e] - tok * D;
@@ -432,17 +425,22 @@ cudaError_t launch_shared_decode(const SharedArgs& a, int dtype, cudaStream_t st
     cudaError_t e = once.ensure([]() { return cudaSuccess; }, &sms);
     if (e != cudaSuccess) return e;
     SharedSched sch;
-    if ((e = plan_shared(a, kRows, sms, sch)) != cudaSuccess) return e;
-    if (dtype == FDKV_BF16) {
-        e = a.d == 128 ? launch_part<__nv_bfloat16, 128>(a, sch, st) : launch_part<__nv_bfloat16, 64>(a, sch, st);
-        if (e == cudaSuccess) e = a.d == 128 ? launch_join<__nv_bfloat16, 128>(a, sch, st) : launch_join<__nv_bfloat16, 64>(a, sch, st);
+    const bool tc = a.tmap != nullptr;
+    if ((e = plan_shared(a, tc ? 128 : kRows, sms, sch)) != cudaSuccess) return e;
+    if (tc) {
+        e = launch_shared_tc(a, sch, st);
+        if (e == cudaSuccess) e = launch_join<__nv_bfloat16, 128>(a, sch, st);
+    } else if (dtype == FDKV_BF16) {
+        if (a.d == 128) return cudaErrorNotSupported;  // (no tensor map of the arena)
+        e = launch_part<__nv_bfloat16, 64>(a, sch, st);
+        if (e == cudaSuccess) e = launch_join<__nv_bfloat16, 64>(a, sch, st);
     } else {
         e = a.d == 128 ? launch_part<float, 128>(a, sch, st) : launch_part<float, 64>(a, sch, st);
         if (e == cudaSuccess) e = a.d == 128 ? launch_join<float, 128>(a, sch, st) : launch_join<float, 64>(a, sch, st);
     }
     if (e != cudaSuccess) return e;
     count_launch(2);
-    count_kernel(FDKV_KERNEL_SHARED_PORTABLE);
+    count_kernel(tc ? FDKV_KERNEL_SHARED_TC : FDKV_KERNEL_SHARED_PORTABLE);
     return cudaGetLastError();
 }
 

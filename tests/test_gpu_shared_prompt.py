@@ -71,6 +71,25 @@ def test_long_prompts_of_every_mode(hkv, modes):
     p.close()
 
 
+def test_blocks_that_walk_many_tiles_of_heads_in_different_modes():
+    """Some twenty tiles per block, whose range runs from a head in one mode into a head in another (the ring of shared memory goes round several
+    times in either), with calls of two contexts behind one another and nothing that waits between."""
+    a = Prompt(41000, 4, 8, 128, BF, modes=[0, 1, 2, 1, 0, 0, 1, 2], keep=(1, 16), max_batch=8, seed=21)
+    b = Prompt(33333, 8, 8, 128, BF, block=4, modes=[1, 2, 2, 0, 1, 1, 0, 1], keep=(1, 32), max_batch=18, seed=22)
+    calls = []
+    for p, layer, n in ((a, 1, 8), (b, 3, 17)):
+        tails = random_tails(p, [(5 * i) % 40 for i in range(n)])
+        put_tails(p, layer, list(range(n)), tails)
+        calls.append((p, layer, list(range(n)), p.new(n, p.G * p.hkv, 128), tails))
+    torch.cuda.synchronize()
+    outs = [[p.ctx.decode_attn_shared(layer, 0, seqs, q) for p, layer, seqs, q, _ in calls] for _ in range(20)]
+    torch.cuda.synchronize()
+    for i, (p, layer, seqs, q, tails) in enumerate(calls):
+        p.check(outs[0][i], layer, q, tails)
+        assert all(torch.equal(o[i], outs[0][i]) for o in outs)
+        p.close()
+
+
 def test_context_with_more_units_than_the_packed_lists_serve():
     """More than 1 024 (slots x KV heads): the residual lists keep their portable layout."""
     p = Prompt(1111, 4, 3, 128, BF, max_batch=400, max_tail=20, modes=[1, 0, 2], seed=3)
