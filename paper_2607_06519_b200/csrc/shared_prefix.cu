@@ -215,7 +215,7 @@ struct SharedSeqs {
     int32_t slot[NB], len[NB];  // len counts this call's append
 };
 
-constexpr int kJoinWarps = 4;
+constexpr int kJoinWarps = 8;
 
 // grid (Hkv, batch).  D / 8 lanes share a tail token, eight channels each; every such lane group keeps a softmax state of its own,
 // joined through shared memory with the prompt's parts.  The tails, q and the new rows are read before the dependency wait: the
@@ -226,6 +226,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(SharedArgs
     constexpr int LPT = D / 8, TPI = 32 / LPT, U = sizeof(T) == 4 || G == 8 ? 2 : 4;
     __shared__ __align__(16) float s_acc[kJoinWarps][G][D];
     __shared__ float s_m[kJoinWarps][G], s_l[kJoinWarps][G];
+    constexpr int JW = kJoinWarps * 32 / (G * D / 4) > 1 ? kJoinWarps * 32 / (G * D / 4) - 1 : 1;
+    __shared__ float4 j_acc[JW][G * D / 4];
+    __shared__ float2 j_ml[JW][G * D / 4];
     const int h = blockIdx.x, b = blockIdx.y;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LPT, c0 = lane % LPT * 8;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -320,33 +323,70 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(SharedArgs
             if (lane == 0) { s_m[warp][g] = M; s_l[warp][g] = l[g]; }
         }
     }
+    // ---- the blocks whose ranges meet the item of the unit's rows (row tiles hold whole sequences) ----
+    const int row0 = b * G, u = h * sch.groups + row0 / sch.row_tile, r0 = row0 % sch.row_tile;
+    int c_lo = 0;
+    for (int step = 128; step; step >>= 1)
+        if (c_lo + step < sch.ncta && sch.start[c_lo + step] <= u * sch.tiles) c_lo += step;
+    int c_hi = c_lo;  // the last block that starts before the item's end
+    for (int step = 128; step; step >>= 1)
+        if (c_hi + step < sch.ncta && sch.start[c_hi + step] < (u + 1) * sch.tiles) c_hi += step;
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the prompt's parts
-    // ---- four channels of a head per thread: the tail's states, then the parts of the row ----
-    for (int i = threadIdx.x; i < G * D / 4; i += kJoinWarps * 32) {
-        const int g = i % G, c4 = i / G;
+    // ---- four channels of a head per thread, the parts spread over as many threads as there are: six at a time on their way ----
+    constexpr int ITEMS = G * D / 4, WAYS = kJoinWarps * 32 / ITEMS > 0 ? kJoinWarps * 32 / ITEMS : 1, BATCH = 6;
+    for (int i0 = 0; i0 < ITEMS * WAYS; i0 += kJoinWarps * 32) {
+        const int i = (i0 + (int)threadIdx.x) % ITEMS, way = (i0 + (int)threadIdx.x) / ITEMS, g = i % G, c4 = i / G;
         float M = -INFINITY, L = 0.f;
         float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i0 + (int)threadIdx.x < ITEMS * WAYS) {
+            const int64_t stride = shared_part_floats(sch.row_tile, D);
+            const float* const p0 = a.partials + u * stride;
+            for (int c = c_lo + way; c <= c_hi; c += BATCH * WAYS) {
+                float pm[BATCH], pl[BATCH];
+                float4 po[BATCH];
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) {
+                    const int cc = c + k * WAYS;
+                    const float* const part = p0 + (cc <= c_hi ? cc : c) * stride;
+                    pm[k] = cc <= c_hi ? __ldcg(part + (int64_t)sch.row_tile * D + r0 + g) : -INFINITY;
+                    pl[k] = __ldcg(part + (int64_t)sch.row_tile * (D + 1) + r0 + g);
+                    po[k] = __ldcg(reinterpret_cast<const float4*>(part + ((int64_t)c4 * sch.row_tile + r0 + g) * 4));
+                }
+                float mn = M;
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) mn = fmaxf(mn, pm[k]);
+                const float ref = mn == -INFINITY ? 0.f : mn, f0 = __expf(M - ref);
+                L *= f0;
+                A.x *= f0; A.y *= f0; A.z *= f0; A.w *= f0;
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) {
+                    const float f = __expf(pm[k] - ref);
+                    L = fmaf(pl[k], f, L);
+                    A.x = fmaf(po[k].x, f, A.x); A.y = fmaf(po[k].y, f, A.y); A.z = fmaf(po[k].z, f, A.z); A.w = fmaf(po[k].w, f, A.w);
+                }
+                M = mn;
+            }
+        }
         auto add = [&](float pm, float pl, const float4& o) {
-            if (pm == -INFINITY) return;
-            const float mn = fmaxf(M, pm), f0 = M == -INFINITY ? 0.f : __expf(M - mn), f1 = __expf(pm - mn);
+            const float mn = fmaxf(M, pm), ref = mn == -INFINITY ? 0.f : mn, f0 = __expf(M - ref), f1 = __expf(pm - ref);
             L = L * f0 + pl * f1;
             A.x = A.x * f0 + o.x * f1; A.y = A.y * f0 + o.y * f1; A.z = A.z * f0 + o.z * f1; A.w = A.w * f0 + o.w * f1;
             M = mn;
         };
+        if constexpr (WAYS > 1) {  // (one round: every thread has at most one item)
+            if (way > 0 && way < WAYS) {
+                j_acc[way - 1][i] = A;
+                j_ml[way - 1][i] = make_float2(M, L);
+            }
+            __syncthreads();
+            if (way > 0) return;
+#pragma unroll
+            for (int w = 1; w < WAYS; ++w) add(j_ml[w - 1][i].x, j_ml[w - 1][i].y, j_acc[w - 1][i]);
+        }
+        if (i0 + (int)threadIdx.x >= ITEMS * WAYS) return;
 #pragma unroll
         for (int w = 0; w < kJoinWarps; ++w) add(s_m[w][g], s_l[w][g], *reinterpret_cast<const float4*>(&s_acc[w][g][c4 * 4]));
-        const int row = b * G + g, u = h * sch.groups + row / sch.row_tile, r = row % sch.row_tile;
-        // the blocks whose ranges meet the item's tiles
-        const int lo = u * sch.tiles, hi = lo + sch.tiles;
-        int c = 0;
-        for (int step = 128; step; step >>= 1)
-            if (c + step < sch.ncta && sch.start[c + step] <= lo) c += step;
-        for (; c < sch.ncta && sch.start[c] < hi; ++c) {
-            const float* const part = a.partials + (int64_t)(c + u) * shared_part_floats(sch.row_tile, D);
-            add(__ldcg(part + (int64_t)sch.row_tile * D + r), __ldcg(part + (int64_t)sch.row_tile * (D + 1) + r),
-                __ldcg(reinterpret_cast<const float4*>(part + ((int64_t)c4 * sch.row_tile + r) * 4)));
-        }
         const float inv = L > 0.f ? 1.f / L : 0.f;
         const int64_t o = ((int64_t)b * a.Hq + h * G + g) * D + c4 * 4;
         if (a.out_dtype == FDKV_BF16) {

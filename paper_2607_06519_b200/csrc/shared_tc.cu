@@ -201,29 +201,58 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 continue;
             }
             const int slices = (ud.T + kResTile - 1) / kResTile;
+            const int k_end = ud.k_off[slices], v_end = ud.v_off ? ud.v_off[slices] : k_end;
             const uint32_t flip = ud.sign < 0.f ? 0x8000u : 0u;
             const bool tokens = ud.res_kind == 1, packed = !tokens && !ud.k_val, twice = ud.sign == 2.f && !a.twice;
-            constexpr int kPF = 8;  // entries a lane requests before it waits for the slot
-            auto fill = [&](int tile, bool is_v) {
-                pass_rows();
-                const int32_t* const off = is_v && ud.v_off ? ud.v_off : ud.k_off;
+            // The fills of the run in ring order: K of tile 0, then K of tile j + 1 and V of tile j in turn.  A fill's entries are requested
+            // when the one before is done and land while the ring makes room, out of L2, where a request two tiles ahead has put them.
+            constexpr int kPF = 12;  // entries a lane requests ahead (the rest are loaded when they are used)
+            int rk[3] = {}, rv[3] = {};  // bounds of this warp's two slices in either list, one tile per lane
+            auto ranges = [&](bool is_v, int j, int& e0, int& mid, int& e1) {
+                int(&x)[3] = is_v ? rv : rk;
+                if ((j & 31) == 0) {
+                    const int32_t* const off = is_v && ud.v_off ? ud.v_off : ud.k_off;
+                    const int s0 = min(slices, (r.t0 + j + lane) * 8 + 2 * w);
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) x[i] = off[min(slices, s0 + i)];
+                }
+                e0 = __shfl_sync(0xFFFFFFFFu, x[0], j & 31);
+                mid = __shfl_sync(0xFFFFFFFFu, x[1], j & 31);
+                e1 = __shfl_sync(0xFFFFFFFFu, x[2], j & 31);
+            };
+            uint32_t pe[kPF];
+            int e0 = 0, mid = 0, e1 = 0;
+            auto entry = [&](const int32_t* idx, const void* val, int e) {  // value in the low half, place in a slice's tile (in elements) in the high one
+                const uint32_t x = (uint32_t)idx[e];
+                if (packed) return x;
+                uint32_t v = reinterpret_cast<const uint16_t*>(val)[e];
+                if (twice) v = __bfloat16_as_ushort(__float2bfloat16_rn(2.f * __uint_as_float(v << 16)));
+                const uint32_t row = x >> 7 & 15, ch = x & 127;  // (flat index token * 128 + channel)
+                return v | ((ch >> 6) * 1024 + row * 64 + (((ch >> 3 & 7) ^ (row & 7)) << 3) + (ch & 7)) << 16;
+            };
+            auto is_v_of = [&](int f) { return f > 0 && ((f & 1) == 0 || f == 2 * r.n - 1); };
+            auto tile_of = [&](int f) { return f == 2 * r.n - 1 ? r.n - 1 : f & 1 ? (f + 1) >> 1 : f == 0 ? 0 : (f >> 1) - 1; };
+            auto request = [&](int f) {
+                if (f >= 2 * r.n) return;
+                const bool is_v = is_v_of(f);
+                ranges(is_v, tile_of(f), e0, mid, e1);
+                if (tokens) return;
                 const int32_t* const idx = is_v && ud.v_idx ? ud.v_idx : ud.k_idx;
                 const void* const val = is_v ? ud.v_val : ud.k_val;
-                const int s0 = min(slices, tile * 8 + 2 * w);
-                const int e0 = off[s0], mid = off[min(slices, s0 + 1)], e1 = off[min(slices, s0 + 2)];
-                uint32_t pe[kPF];
-                auto entry = [&](int e) {  // value in the low half, place in a slice's tile (in elements) in the high one
-                    const uint32_t x = (uint32_t)idx[e];
-                    if (packed) return x ^ flip;
-                    uint32_t v = reinterpret_cast<const uint16_t*>(val)[e];
-                    if (twice) v = __bfloat16_as_ushort(__float2bfloat16_rn(2.f * __uint_as_float(v << 16)));
-                    const uint32_t row = x >> 7 & 15, ch = x & 127;  // (flat index token * 128 + channel)
-                    return (v ^ flip) | ((ch >> 6) * 1024 + row * 64 + (((ch >> 3 & 7) ^ (row & 7)) << 3) + (ch & 7)) << 16;
-                };
-                if (!tokens)
 #pragma unroll
-                    for (int i = 0; i < kPF; ++i)
-                        if (e0 + lane + 32 * i < e1) pe[i] = entry(e0 + lane + 32 * i);
+                for (int i = 0; i < kPF; ++i)
+                    if (e0 + lane + 32 * i < e1) pe[i] = entry(idx, val, e0 + lane + 32 * i);
+                // (about where the list is two tiles on: the slices' counts are much alike)
+                const int ahead = e0 + (e1 - e0) * 8 + lane * 32;
+                const int last = is_v ? v_end : k_end;
+                if (lane * 32 < (e1 - e0) + 64 && ahead < last) asm volatile("prefetch.global.L2 [%0];" ::"l"(idx + ahead));
+            };
+            request(0);
+            for (int f = 0; f < 2 * r.n; ++f) {
+                const bool is_v = is_v_of(f);
+                const int32_t* const idx = is_v && ud.v_idx ? ud.v_idx : ud.k_idx;
+                const void* const val = is_v ? ud.v_val : ud.k_val;
+                pass_rows();
                 const uint32_t base = slot0 + sl * kSlotBytes + w * 4096;
                 mb_wait(sm0 + oEmpty + 8 * sl, ph ^ 1u, abort_flag, a.status);
 #pragma unroll
@@ -242,21 +271,26 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 } else {
                     auto put = [&](int e, uint32_t x) {
                         const uint32_t o = x >> 16 << 1;
-                        st_u16(base + (o >> 11) * kHalf + (o & 2047) + (e >= mid ? 2048 : 0), x);
+                        st_u16(base + (o >> 11) * kHalf + (o & 2047) + (e >= mid ? 2048 : 0), x ^ flip);
                     };
 #pragma unroll
                     for (int i = 0; i < kPF; ++i)
                         if (e0 + lane + 32 * i < e1) put(e0 + lane + 32 * i, pe[i]);
-                    for (int e = e0 + lane + 32 * kPF; e < e1; e += 32) put(e, entry(e));
+                    for (int eb = e0 + 32 * kPF; eb < e1; eb += 128) {  // dense slices: four in flight
+                        uint32_t x[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (eb + lane + 32 * i < e1) x[i] = entry(idx, val, eb + lane + 32 * i);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (eb + lane + 32 * i < e1) put(eb + lane + 32 * i, x[i]);
+                    }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mb_arrive(sm0 + oFull + 8 * sl);
                 advance();
-            };
-            for (int j = -1; j < r.n; ++j) {
-                if (j + 1 < r.n) fill(r.t0 + j + 1, false);
-                if (j >= 0) fill(r.t0 + j, true);
+                request(f + 1);
             }
         }
     } else {
