@@ -39,6 +39,30 @@ __device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64
         "r"(tmem_a), "l"(db), "n"(IDESC), "r"(acc)
         : "memory");
 }
+__device__ __forceinline__ bool elect_one() {
+    uint32_t x;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(x));
+    return x != 0;
+}
+// All lanes wait for a barrier's phase; false when the block has given up.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, int32_t* status) {
+    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity) != 0)) return true;
+    mb_wait(bar, parity, abort_flag, status);
+    __syncwarp();
+    return !__any_sync(0xFFFFFFFFu, *abort_flag != 0);
+}
+// 32 bytes past the L1 cache, in one request where the address allows it (the caller's tensors are aligned to 16 bytes)
+__device__ __forceinline__ void ldcg32(const void* p, uint32_t* x) {
+    if (reinterpret_cast<uint64_t>(p) & 16) {
+        const uint4 a = __ldcg(reinterpret_cast<const uint4*>(p)), b = __ldcg(reinterpret_cast<const uint4*>(p) + 1);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        return;
+    }
+    asm volatile("ld.global.cg.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7])
+                 : "l"(p)
+                 : "memory");
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -73,7 +97,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sm0 = s_u32(smem), slot0 = sm0 + kHeader;
     volatile uint32_t* const abort_flag = reinterpret_cast<volatile uint32_t*>(smem + oAbort);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (uniform to the compiler)
     if (sm0 & 1023u) {  // the swizzled tiles need 1024-byte alignment; report instead of computing garbage
         if (threadIdx.x == 0) atomicMax(a.status, (int32_t)kFlagCountMismatch);
         return;
@@ -140,49 +164,51 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             }
         }
     } else if (warp == 9) {
-        if (lane == 0) {
-            int it = 0;
-            uint32_t qph = 0;
-            while (next_run(sch, g, g_end, r)) {
-                const bool resid = a.desc[r.h].mode == FDKV_MODE_RESIDUAL;
-                mb_wait(sm0 + oQ, qph, abort_flag, a.status);
-                qph ^= 1u;
-                if (*abort_flag) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                // the products of one tile of rows, then of its entries
-                auto scores = [&](int b) {
-                    for (int e = 0; e < (resid ? 2 : 1); ++e) {
-                        mb_wait(sm0 + oFull + 8 * sl, ph, abort_flag, a.status);
-                        if (*abort_flag) return;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint64_t d = smem_desc(slot0 + sl * kSlotBytes);
+        // The whole warp walks the loop and one lane issues, so that descriptors and addresses stay in uniform registers: with
+        // the loop behind `if (lane == 0)` issuing a tile's products took 2 700 cycles, more than the softmax.
+        const bool leader = elect_one();
+        int it = 0;
+        uint32_t qph = 0;
+        bool ok = true;
+        while (ok && next_run(sch, g, g_end, r)) {
+            const int parts = a.desc[r.h].mode == FDKV_MODE_RESIDUAL ? 2 : 1;  // a tile's rows, then its entries
+            ok = wait_warp(sm0 + oQ, qph, abort_flag, a.status);
+            qph ^= 1u;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            auto scores = [&](int b) {
+                for (int e = 0; e < parts && ok; ++e) {
+                    ok = wait_warp(sm0 + oFull + 8 * sl, ph, abort_flag, a.status);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t d = smem_desc(slot0 + sl * kSlotBytes);
+                    const uint32_t ts = tmem + cS + b * 128;
+                    if (leader && ok) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            umma_ts<kIdescS>(tmem + cS + b * 128, tmem + cQ + 8 * k, d + (k >> 2) * (kHalf >> 4) + (k & 3) * 2, e > 0 || k > 0);
+                        for (int k = 0; k < 8; ++k) umma_ts<kIdescS>(ts, tmem + cQ + 8 * k, d + (k >> 2) * (kHalf >> 4) + (k & 3) * 2, e > 0 || k > 0);
                         umma_commit(sm0 + oEmpty + 8 * sl);
-                        advance();
+                        if (e + 1 == parts) umma_commit(sm0 + oS + 8 * b);
                     }
-                    umma_commit(sm0 + oS + 8 * b);
-                };
-                scores(it & 1);
-                for (int j = 0; j < r.n; ++j, ++it) {
-                    if (j + 1 < r.n) scores((it + 1) & 1);
-                    mb_wait(sm0 + oP + 8 * (it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, a.status);
-                    if (*abort_flag) break;
-                    for (int e = 0; e < (resid ? 2 : 1); ++e) {
-                        mb_wait(sm0 + oFull + 8 * sl, ph, abort_flag, a.status);
-                        if (*abort_flag) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint64_t d = smem_desc_sw128(slot0 + sl * kSlotBytes, kHalf, 1024);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            umma_ts<kIdescO>(tmem + cO, tmem + cS + (it & 1) * 128 + 8 * k, d + k * (2048 >> 4), j > 0 || e > 0 || k > 0);
-                        umma_commit(sm0 + oEmpty + 8 * sl);
-                        advance();
-                    }
-                    umma_commit(sm0 + oO + 8 * (it & 1));
+                    __syncwarp();
+                    advance();
                 }
-                if (*abort_flag) break;
+            };
+            if (ok) scores(it & 1);
+            for (int j = 0; j < r.n && ok; ++j, ++it) {
+                if (j + 1 < r.n) scores((it + 1) & 1);
+                ok = ok && wait_warp(sm0 + oP + 8 * (it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, a.status);
+                for (int e = 0; e < parts && ok; ++e) {
+                    ok = wait_warp(sm0 + oFull + 8 * sl, ph, abort_flag, a.status);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t d = smem_desc_sw128(slot0 + sl * kSlotBytes, kHalf, 1024);
+                    const uint32_t tp = tmem + cS + (it & 1) * 128;
+                    if (leader && ok) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) umma_ts<kIdescO>(tmem + cO, tp + 8 * k, d + k * (2048 >> 4), j > 0 || e > 0 || k > 0);
+                        umma_commit(sm0 + oEmpty + 8 * sl);
+                        if (e + 1 == parts) umma_commit(sm0 + oO + 8 * (it & 1));
+                    }
+                    __syncwarp();
+                    advance();
+                }
             }
         }
     } else if (warp >= 4) {
@@ -305,17 +331,17 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             const float ks = uscale * (0.08838834764831845f * 1.4426950408889634f);  // / sqrt(128), in powers of two
             {
                 const int row = r.row0 + (int)threadIdx.x, b = row / a.G;
-                const uint4* const src = reinterpret_cast<const uint4*>(a.q) + ((int64_t)b * a.Hq + r.h * a.G + (row - b * a.G)) * 16;
+                const char* const src = reinterpret_cast<const char*>(a.q) + (((int64_t)b * a.Hq + r.h * a.G + (row - b * a.G)) << 8);
+                uint32_t x[2][32];
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t x[32];
+                for (int i = 0; i < 8; ++i) {
+                    if ((int)threadIdx.x < rows) ldcg32(src + 32 * i, &x[i >> 2][8 * (i & 3)]);
+                    else
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint4 v = (int)threadIdx.x < rows ? __ldcg(src + 8 * half + i) : make_uint4(0u, 0u, 0u, 0u);
-                        x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
-                    }
-                    tmem_st32(tq + cQ + 32 * half, x);
+                        for (int k = 0; k < 8; ++k) x[i >> 2][8 * (i & 3) + k] = 0u;
                 }
+                tmem_st32(tq + cQ, x[0]);
+                tmem_st32(tq + cQ + 32, x[1]);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();

@@ -90,6 +90,23 @@ def test_blocks_that_walk_many_tiles_of_heads_in_different_modes():
         p.close()
 
 
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (F, 64)])
+def test_tensors_aligned_to_sixteen_bytes_only(dtype, d):
+    p = Prompt(300, 4, 2, d, dtype, max_batch=5, seed=23)
+    n = 16 // torch.tensor([], dtype=dtype).element_size()
+
+    def shifted(*shape):
+        return torch.cat([p.new(n), p.new(*shape).flatten()])[n:].view(shape)
+
+    seqs, tails = [1, 2, 4], random_tails(p, [20, 0, 3])
+    put_tails(p, 1, seqs, tails)
+    q, kn, vn, out = shifted(3, 8, d), shifted(3, 2, d), shifted(3, 2, d), shifted(3, 8, d)
+    assert q.data_ptr() % 32 == kn.data_ptr() % 32 == out.data_ptr() % 32 == 16
+    p.ctx.decode_attn_shared(1, 0, seqs, q, kn, vn, out=out)
+    p.check(out, 1, q, [(torch.cat([k, kn[b:b + 1]]), torch.cat([v, vn[b:b + 1]])) for b, (k, v) in enumerate(tails)])
+    p.close()
+
+
 def test_context_with_more_units_than_the_packed_lists_serve():
     """More than 1 024 (slots x KV heads): the residual lists keep their portable layout."""
     p = Prompt(1111, 4, 3, 128, BF, max_batch=400, max_tail=20, modes=[1, 0, 2], seed=3)
