@@ -1,13 +1,14 @@
 // The prompt part of decode attention on one shared prompt, bf16 / head_dim 128 (see shared_prefix.cu): the query rows of all
 // sequences of a KV head fill the rows of tcgen05 products, so that a tile of the compressed prompt is read once and used by up to 128 rows.
 //
-// A persistent block of ten warps per SM walks a range of the flat (KV head, row group, 128-token tile) list:
-//   warp 8     TMA producer: the tile's K and V rows (2 x 64 channels x 128 tokens, 128-byte swizzle)
-//   warps 4-7  residual units: the tile's kept entries, scattered into a zeroed tile of the same layout (32 tokens per warp)
-//   warp 9     issues S = Q K^T (Q from tensor memory, K-major K) and O += P V (P from tensor memory, MN-major V).  Residual units add
+// A persistent block per SM walks a range of the flat (KV head, row group, 128-token tile) list:
+//   warp 12    TMA producer: the tile's K and V rows (2 x 64 channels x 128 tokens, 128-byte swizzle)
+//   warps 4-11 residual units: the tile's kept entries of K (4-7) and V (8-11), scattered into a zeroed tile of the same layout (32
+//              tokens per warp)
+//   warp 13    issues S = Q K^T (Q from tensor memory, K-major K) and O += P V (P from tensor memory, MN-major V).  Residual units add
 //              the products with the entries' tiles into the same accumulators, so that the correction is exact in float32
 //   warps 0-3  softmax: thread = query row.  S is read from tensor memory, P = exp2(S - max) rounded to bf16 takes its place; the
-//              running maximum only moves, and O is only rescaled, where a score passes it by more than 2^8
+//              running maximum only moves, and O is only rescaled, where a score passes it by more than 2^16
 // All tiles, rows and entries alike, go through one ring of 32 KiB slots in the order in which the products use them: K of the next
 // tile lies before V of this one, so that the next S is formed while the softmax of this one runs (S has two accumulators).
 // P in bf16: a probability is off by 2^-8 at most, each its own way; the sums l are those of the unrounded ones.
@@ -20,13 +21,14 @@ namespace fdkv {
 
 namespace {
 
-constexpr int kThreads = 320;
+constexpr int kThreads = 448;
 constexpr int kSlots = 7, kSlotBytes = 32768, kHalf = 16384;
+constexpr float kLazy = 16.f;  // (powers of two)
 constexpr int kHeader = 1024;
 constexpr int kSmem = kHeader + kSlots * kSlotBytes;
 static_assert(kSmem <= 227 * 1024, "shared memory budget");
 // header
-constexpr int oFull = 0, oEmpty = 64, oS = 128, oP = 144, oO = 160, oQ = 176, oAbort = 184, oTmem = 188;
+constexpr int oFull = 0, oEmpty = 64, oS = 128, oP = 144, oO = 160, oQ = 176, oAbort = 184, oTmem = 188, oRun = 192;
 // tensor memory columns
 constexpr uint32_t cS = 0, cO = 256, cQ = 384;
 constexpr uint32_t kIdescS = umma_idesc(128, 128, false), kIdescO = umma_idesc(128, 128, false) | (1u << 16);  // (B of the second product is MN-major)
@@ -68,6 +70,26 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// (x, y) = (a, b) * s + t, two at a time
+__device__ __forceinline__ void scaled2(uint32_t a, uint32_t b, float s, float t, float& x, float& y) {
+    asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %4};\n\tmov.b64 r, {%5, %5};\n\tfma.rn.f32x2 p, p, q, r;\n\tmov.b64 {%0, %1}, p;\n\t}"
+        : "=f"(x), "=f"(y)
+        : "r"(a), "r"(b), "f"(s), "f"(t));
+}
+__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tadd.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+                   "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -97,6 +119,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sm0 = s_u32(smem), slot0 = sm0 + kHeader;
     volatile uint32_t* const abort_flag = reinterpret_cast<volatile uint32_t*>(smem + oAbort);
+    volatile uint32_t* const run_no = reinterpret_cast<volatile uint32_t*>(smem + oRun);  // runs that the producer has begun
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (uniform to the compiler)
     if (sm0 & 1023u) {  // the swizzled tiles need 1024-byte alignment; report instead of computing garbage
         if (threadIdx.x == 0) atomicMax(a.status, (int32_t)kFlagCountMismatch);
@@ -104,7 +127,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < kSlots; ++s) {
-            mb_init(sm0 + oFull + 8 * s, 5);  // the producer and the entries' warps: both pass every slot, so that no role is a round ahead of or behind another
+            mb_init(sm0 + oFull + 8 * s, 4);  // the four warps that fill a tile of entries, or as many arrivals of the producer
             mb_init(sm0 + oEmpty + 8 * s, 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -115,9 +138,10 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
         }
         mb_init(sm0 + oQ, 4);
         *abort_flag = 0;
+        *run_no = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 9) {
+    if (warp == 13) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sm0 + oTmem), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -135,152 +159,136 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
         if (++sl == kSlots) { sl = 0; ph ^= 1u; }
     };
 
-    if (warp == 8) {
-        if (lane == 0) {
-            while (next_run(sch, g, g_end, r)) {
-                const UnitDesc* const ud = a.desc + r.h;
-                const bool resid = ud->mode == FDKV_MODE_RESIDUAL;
-                const uint64_t arena = reinterpret_cast<uint64_t>(a.arena_base);
-                const int krow = (int)((reinterpret_cast<uint64_t>(ud->k_rows) - arena) >> 8), vrow = (int)((reinterpret_cast<uint64_t>(ud->v_rows) - arena) >> 8);
-                auto load = [&](int row) {
-                    const uint32_t full = sm0 + oFull + 8 * sl, dst = slot0 + sl * kSlotBytes;
-                    mb_wait(sm0 + oEmpty + 8 * sl, ph ^ 1u, abort_flag, a.status);
-                    if (!*abort_flag) {
-                        mb_expect_tx(full, kSlotBytes);
-                        tma_2d(dst, &tmap, 0, row, full);
-                        tma_2d(dst + kHalf, &tmap, 64, row, full);
-                    }
-                    advance();
-                    if (resid) {
+    if (warp >= 12) {
+        if (warp == 12) {
+            if (lane == 0) {
+                uint32_t runs = 0;
+                while (next_run(sch, g, g_end, r)) {
+                    *run_no = ++runs;
+                    const UnitDesc* const ud = a.desc + r.h;
+                    const bool resid = ud->mode == FDKV_MODE_RESIDUAL;
+                    const uint64_t arena = reinterpret_cast<uint64_t>(a.arena_base);
+                    const int krow = (int)((reinterpret_cast<uint64_t>(ud->k_rows) - arena) >> 8), vrow = (int)((reinterpret_cast<uint64_t>(ud->v_rows) - arena) >> 8);
+                    auto load = [&](int row) {
+                        const uint32_t full = sm0 + oFull + 8 * sl, dst = slot0 + sl * kSlotBytes;
                         mb_wait(sm0 + oEmpty + 8 * sl, ph ^ 1u, abort_flag, a.status);
-                        mb_arrive(sm0 + oFull + 8 * sl);
+                        if (!*abort_flag) {
+                            mb_expect_tx(full, kSlotBytes);
+                            tma_2d(dst, &tmap, 0, row, full);
+                            tma_2d(dst + kHalf, &tmap, 64, row, full);
+                            for (int i = 0; i < 3; ++i) mb_arrive(full);
+                        }
+                        advance();
+                        if (resid) advance();
+                    };
+                    for (int j = -1; j < r.n; ++j) {
+                        if (j + 1 < r.n) load(krow + (r.t0 + j + 1) * kSharedTile);
+                        if (j >= 0) load(vrow + (r.t0 + j) * kSharedTile);
+                    }
+                }
+            }
+        } else if (warp == 13) {
+            // The whole warp walks the loop and one lane issues, so that descriptors and addresses stay in uniform registers: with
+            // the loop behind `if (lane == 0)` issuing a tile's products took 2 700 cycles, more than the softmax.
+            const bool leader = elect_one();
+            int it = 0;
+            uint32_t qph = 0;
+            bool ok = true;
+            while (ok && next_run(sch, g, g_end, r)) {
+                const int parts = a.desc[r.h].mode == FDKV_MODE_RESIDUAL ? 2 : 1;  // a tile's rows, then its entries
+                ok = wait_warp(sm0 + oQ, qph, abort_flag, a.status);
+                qph ^= 1u;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                auto scores = [&](int b) {
+                    for (int e = 0; e < parts && ok; ++e) {
+                        ok = wait_warp(sm0 + oFull + 8 * sl, ph, abort_flag, a.status);
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint64_t d = smem_desc(slot0 + sl * kSlotBytes);
+                        const uint32_t ts = tmem + cS + b * 128;
+                        if (leader && ok) {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) umma_ts<kIdescS>(ts, tmem + cQ + 8 * k, d + (k >> 2) * (kHalf >> 4) + (k & 3) * 2, e > 0 || k > 0);
+                            umma_commit(sm0 + oEmpty + 8 * sl);
+                            if (e + 1 == parts) umma_commit(sm0 + oS + 8 * b);
+                        }
+                        __syncwarp();
                         advance();
                     }
                 };
-                for (int j = -1; j < r.n; ++j) {
-                    if (j + 1 < r.n) load(krow + (r.t0 + j + 1) * kSharedTile);
-                    if (j >= 0) load(vrow + (r.t0 + j) * kSharedTile);
-                }
-            }
-        }
-    } else if (warp == 9) {
-        // The whole warp walks the loop and one lane issues, so that descriptors and addresses stay in uniform registers: with
-        // the loop behind `if (lane == 0)` issuing a tile's products took 2 700 cycles, more than the softmax.
-        const bool leader = elect_one();
-        int it = 0;
-        uint32_t qph = 0;
-        bool ok = true;
-        while (ok && next_run(sch, g, g_end, r)) {
-            const int parts = a.desc[r.h].mode == FDKV_MODE_RESIDUAL ? 2 : 1;  // a tile's rows, then its entries
-            ok = wait_warp(sm0 + oQ, qph, abort_flag, a.status);
-            qph ^= 1u;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            auto scores = [&](int b) {
-                for (int e = 0; e < parts && ok; ++e) {
-                    ok = wait_warp(sm0 + oFull + 8 * sl, ph, abort_flag, a.status);
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t d = smem_desc(slot0 + sl * kSlotBytes);
-                    const uint32_t ts = tmem + cS + b * 128;
-                    if (leader && ok) {
+                if (ok) scores(it & 1);
+                for (int j = 0; j < r.n && ok; ++j, ++it) {
+                    if (j + 1 < r.n) scores((it + 1) & 1);
+                    ok = ok && wait_warp(sm0 + oP + 8 * (it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, a.status);
+                    for (int e = 0; e < parts && ok; ++e) {
+                        ok = wait_warp(sm0 + oFull + 8 * sl, ph, abort_flag, a.status);
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint64_t d = smem_desc_sw128(slot0 + sl * kSlotBytes, kHalf, 1024);
+                        const uint32_t tp = tmem + cS + (it & 1) * 128;
+                        if (leader && ok) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) umma_ts<kIdescS>(ts, tmem + cQ + 8 * k, d + (k >> 2) * (kHalf >> 4) + (k & 3) * 2, e > 0 || k > 0);
-                        umma_commit(sm0 + oEmpty + 8 * sl);
-                        if (e + 1 == parts) umma_commit(sm0 + oS + 8 * b);
+                            for (int k = 0; k < 8; ++k) umma_ts<kIdescO>(tmem + cO, tp + 8 * k, d + k * (2048 >> 4), j > 0 || e > 0 || k > 0);
+                            umma_commit(sm0 + oEmpty + 8 * sl);
+                            if (e + 1 == parts) umma_commit(sm0 + oO + 8 * (it & 1));
+                        }
+                        __syncwarp();
+                        advance();
                     }
-                    __syncwarp();
-                    advance();
-                }
-            };
-            if (ok) scores(it & 1);
-            for (int j = 0; j < r.n && ok; ++j, ++it) {
-                if (j + 1 < r.n) scores((it + 1) & 1);
-                ok = ok && wait_warp(sm0 + oP + 8 * (it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, a.status);
-                for (int e = 0; e < parts && ok; ++e) {
-                    ok = wait_warp(sm0 + oFull + 8 * sl, ph, abort_flag, a.status);
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t d = smem_desc_sw128(slot0 + sl * kSlotBytes, kHalf, 1024);
-                    const uint32_t tp = tmem + cS + (it & 1) * 128;
-                    if (leader && ok) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) umma_ts<kIdescO>(tmem + cO, tp + 8 * k, d + k * (2048 >> 4), j > 0 || e > 0 || k > 0);
-                        umma_commit(sm0 + oEmpty + 8 * sl);
-                        if (e + 1 == parts) umma_commit(sm0 + oO + 8 * (it & 1));
-                    }
-                    __syncwarp();
-                    advance();
                 }
             }
         }
     } else if (warp >= 4) {
-        // ---- the residual's tiles: this warp has tokens [32 w, 32 w + 32) of them, two 16-token slices ----
-        const int w = warp - 4;
+        // ---- the residual's tiles of K or of V: this warp has tokens [32 w, 32 w + 32) of them, two 16-token slices ----
+        const int w = warp & 3;
+        const bool is_v = warp >= 8;
+        uint32_t runs = 0;
         while (next_run(sch, g, g_end, r)) {
             const UnitDesc ud = a.desc[r.h];
-            auto pass_rows = [&]() {
-                mb_wait(sm0 + oEmpty + 8 * sl, ph ^ 1u, abort_flag, a.status);
-                __syncwarp();
-                if (lane == 0) mb_arrive(sm0 + oFull + 8 * sl);
-                advance();
-            };
-            if (ud.mode != FDKV_MODE_RESIDUAL) {
-                for (int i = 0; i < 2 * r.n; ++i) pass_rows();
+            const bool resid = ud.mode == FDKV_MODE_RESIDUAL;
+            ++runs;
+            if (!resid) {
+                for (int i = 0; i < 2 * r.n; ++i) advance();
                 continue;
             }
+            // A phase of the ring can be told from the one before, not from the one before that.  Within a run every fourth slot is this
+            // warp's; runs without entries it passes at once, so that it waits until the producer, which has waited for slots all along, is here.
+            for (uint32_t i = 0; *run_no < runs && !*abort_flag; ++i)
+                if (i >= kWaitCap) { *abort_flag = 1; atomicMax(a.status, (int32_t)kFlagTimeout); }
+            __syncwarp();
             const int slices = (ud.T + kResTile - 1) / kResTile;
-            const int k_end = ud.k_off[slices], v_end = ud.v_off ? ud.v_off[slices] : k_end;
             const uint32_t flip = ud.sign < 0.f ? 0x8000u : 0u;
             const bool tokens = ud.res_kind == 1, packed = !tokens && !ud.k_val, twice = ud.sign == 2.f && !a.twice;
-            // The fills of the run in ring order: K of tile 0, then K of tile j + 1 and V of tile j in turn.  A fill's entries are requested
-            // when the one before is done and land while the ring makes room, out of L2, where a request two tiles ahead has put them.
+            const int32_t* const off = is_v && ud.v_off ? ud.v_off : ud.k_off;
+            const int32_t* const idx = is_v && ud.v_idx ? ud.v_idx : ud.k_idx;
+            const void* const val = is_v ? ud.v_val : ud.k_val;
+            const int list_end = off[slices];
+            // A tile's entries are requested when the one before is done and land while the ring makes room, out of L2, where a request
+            // two tiles ahead has put them.
             constexpr int kPF = 12;  // entries a lane requests ahead (the rest are loaded when they are used)
-            int rk[3] = {}, rv[3] = {};  // bounds of this warp's two slices in either list, one tile per lane
-            auto ranges = [&](bool is_v, int j, int& e0, int& mid, int& e1) {
-                int(&x)[3] = is_v ? rv : rk;
-                if ((j & 31) == 0) {
-                    const int32_t* const off = is_v && ud.v_off ? ud.v_off : ud.k_off;
-                    const int s0 = min(slices, (r.t0 + j + lane) * 8 + 2 * w);
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) x[i] = off[min(slices, s0 + i)];
-                }
-                e0 = __shfl_sync(0xFFFFFFFFu, x[0], j & 31);
-                mid = __shfl_sync(0xFFFFFFFFu, x[1], j & 31);
-                e1 = __shfl_sync(0xFFFFFFFFu, x[2], j & 31);
-            };
+            int bounds[3] = {};      // of this warp's two slices, one tile per lane
             uint32_t pe[kPF];
             int e0 = 0, mid = 0, e1 = 0;
-            auto entry = [&](const int32_t* idx, const void* val, int e) {  // value in the low half, place in a slice's tile (in elements) in the high one
-                const uint32_t x = (uint32_t)idx[e];
-                if (packed) return x;
-                uint32_t v = reinterpret_cast<const uint16_t*>(val)[e];
-                if (twice) v = __bfloat16_as_ushort(__float2bfloat16_rn(2.f * __uint_as_float(v << 16)));
-                const uint32_t row = x >> 7 & 15, ch = x & 127;  // (flat index token * 128 + channel)
-                return v | ((ch >> 6) * 1024 + row * 64 + (((ch >> 3 & 7) ^ (row & 7)) << 3) + (ch & 7)) << 16;
-            };
-            auto is_v_of = [&](int f) { return f > 0 && ((f & 1) == 0 || f == 2 * r.n - 1); };
-            auto tile_of = [&](int f) { return f == 2 * r.n - 1 ? r.n - 1 : f & 1 ? (f + 1) >> 1 : f == 0 ? 0 : (f >> 1) - 1; };
-            auto request = [&](int f) {
-                if (f >= 2 * r.n) return;
-                const bool is_v = is_v_of(f);
-                ranges(is_v, tile_of(f), e0, mid, e1);
-                if (tokens) return;
-                const int32_t* const idx = is_v && ud.v_idx ? ud.v_idx : ud.k_idx;
-                const void* const val = is_v ? ud.v_val : ud.k_val;
+            auto request = [&](int j) {
+                if (j >= r.n) return;
+                if ((j & 31) == 0) {
+                    const int s0 = min(slices, (r.t0 + j + lane) * 8 + 2 * w);
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) bounds[i] = off[min(slices, s0 + i)];
+                }
+                e0 = __shfl_sync(0xFFFFFFFFu, bounds[0], j & 31);
+                mid = __shfl_sync(0xFFFFFFFFu, bounds[1], j & 31);
+                e1 = __shfl_sync(0xFFFFFFFFu, bounds[2], j & 31);
+                if (!packed) return;
 #pragma unroll
                 for (int i = 0; i < kPF; ++i)
-                    if (e0 + lane + 32 * i < e1) pe[i] = entry(idx, val, e0 + lane + 32 * i);
+                    if (e0 + lane + 32 * i < e1) pe[i] = (uint32_t)idx[e0 + lane + 32 * i];
                 // (about where the list is two tiles on: the slices' counts are much alike)
                 const int ahead = e0 + (e1 - e0) * 8 + lane * 32;
-                const int last = is_v ? v_end : k_end;
-                if (lane * 32 < (e1 - e0) + 64 && ahead < last) asm volatile("prefetch.global.L2 [%0];" ::"l"(idx + ahead));
+                if (lane * 32 < (e1 - e0) + 64 && ahead < list_end) asm volatile("prefetch.global.L2 [%0];" ::"l"(idx + ahead));
             };
-            request(0);
-            for (int f = 0; f < 2 * r.n; ++f) {
-                const bool is_v = is_v_of(f);
-                const int32_t* const idx = is_v && ud.v_idx ? ud.v_idx : ud.k_idx;
-                const void* const val = is_v ? ud.v_val : ud.k_val;
-                pass_rows();
+            auto fill = [&](int j) {
                 const uint32_t base = slot0 + sl * kSlotBytes + w * 4096;
-                mb_wait(sm0 + oEmpty + 8 * sl, ph ^ 1u, abort_flag, a.status);
+                if (lane == 0) mb_wait(sm0 + oEmpty + 8 * sl, ph ^ 1u, abort_flag, a.status);
+                __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     st_v4(base + (lane + 32 * i) * 16, 0u, 0u, 0u, 0u);
@@ -290,33 +298,55 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 if (tokens) {  // whole rows, half a warp each
                     for (int e = e0 + (lane >> 4); e < e1; e += 2) {
                         const int c = lane & 15, row = idx[e] & 15;
-                        uint4 x = reinterpret_cast<const uint4*>(val)[(int64_t)e * 16 + c];
+                        const uint4 x = reinterpret_cast<const uint4*>(val)[(int64_t)e * 16 + c];
                         const uint32_t f2 = flip | flip << 16;
                         st_v4(base + (c >> 3) * kHalf + (e >= mid ? 2048 : 0) + row * 128 + (((c & 7) ^ (row & 7)) << 4), x.x ^ f2, x.y ^ f2, x.z ^ f2, x.w ^ f2);
                     }
                 } else {
-                    auto put = [&](int e, uint32_t x) {
+                    auto put = [&](int e, uint32_t x) {  // value in the low half, place in the slice's tile (in elements) in the high one
                         const uint32_t o = x >> 16 << 1;
-                        st_u16(base + (o >> 11) * kHalf + (o & 2047) + (e >= mid ? 2048 : 0), x ^ flip);
+                        st_u16(base + (e >= mid ? 2048u : 0u) + o + (o & 2048u) * 7u, x ^ flip);  // (the second 64 channels: kHalf on)
                     };
+                    if (packed) {
 #pragma unroll
-                    for (int i = 0; i < kPF; ++i)
-                        if (e0 + lane + 32 * i < e1) put(e0 + lane + 32 * i, pe[i]);
-                    for (int eb = e0 + 32 * kPF; eb < e1; eb += 128) {  // dense slices: four in flight
-                        uint32_t x[4];
+                        for (int i = 0; i < kPF; ++i)
+                            if (e0 + lane + 32 * i < e1) put(e0 + lane + 32 * i, pe[i]);
+#pragma unroll 1
+                        for (int eb = e0 + 32 * kPF; eb < e1; eb += 128) {  // dense slices: four in flight
+                            uint32_t x[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (eb + lane + 32 * i < e1) x[i] = entry(idx, val, eb + lane + 32 * i);
+                            for (int i = 0; i < 4; ++i)
+                                if (eb + lane + 32 * i < e1) x[i] = (uint32_t)idx[eb + lane + 32 * i];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (eb + lane + 32 * i < e1) put(eb + lane + 32 * i, x[i]);
+                            for (int i = 0; i < 4; ++i)
+                                if (eb + lane + 32 * i < e1) put(eb + lane + 32 * i, x[i]);
+                        }
+                    } else {  // flat indices token * 128 + channel, and values
+#pragma unroll 1
+                        for (int e = e0 + lane; e < e1; e += 32) {
+                            const uint32_t x = (uint32_t)idx[e], row = x >> 7 & 15, ch = x & 127;
+                            uint32_t v = reinterpret_cast<const uint16_t*>(val)[e];
+                            if (twice) v = __bfloat16_as_ushort(__float2bfloat16_rn(2.f * __uint_as_float(v << 16)));
+                            put(e, v | ((ch >> 6) * 1024 + row * 64 + (((ch >> 3 & 7) ^ (row & 7)) << 3) + (ch & 7)) << 16);
+                        }
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mb_arrive(sm0 + oFull + 8 * sl);
                 advance();
-                request(f + 1);
+                request(j + 1);
+            };
+            request(0);
+            for (int j = -1; j < r.n; ++j) {
+                if (j + 1 < r.n) {
+                    advance();
+                    if (is_v) advance(); else fill(j + 1);
+                }
+                if (j >= 0) {
+                    advance();
+                    if (is_v) fill(j); else advance();
+                }
             }
         }
     } else {
@@ -347,66 +377,84 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 __syncwarp();
                 if (lane == 0) mb_arrive(sm0 + oQ);
             }
-            float m = -INFINITY, l = 0.f;
+            float m = -INFINITY;                    // what the exponents are relative to, in powers of two
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            // A score passes the reference by more than 2^kLazy (or there is none yet): the row's sums, its accumulators and what this tile
+            // has of its P are scaled down, by a power of two, so that P stays exactly as it was rounded.
+            auto move_reference = [&](float top, int j, int c) {
+                const float m_new = fmaxf(m, ceilf(top));
+                const float f = ex2(m - m_new);  // (0 at the first scores)
+                m = m_new;
+                if (j == 0 && c == 0) return;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] *= f;
+                const uint32_t tp = tq + cS + (it & 1) * 128;
+#pragma unroll 1
+                for (int k = 0; k < c; ++k) {
+                    uint32_t x[16];
+                    tmem_ld16(tp + 16 * k, x);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = pack2(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xFFFF0000u) * f);
+                    tmem_st16(tp + 16 * k, x);
+                }
+                if (j == 0) return;
+                mb_wait(sm0 + oO + 8 * ((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, abort_flag, a.status);
+                __syncwarp();
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+                for (int k = 0; k < 8; ++k) {
+                    uint32_t o[16];
+                    tmem_ld16(tq + cO + 16 * k, o);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                    tmem_st16(tq + cO + 16 * k, o);
+                }
+            };
             for (int j = 0; j < r.n; ++j, ++it) {
                 const uint32_t ts = tq + cS + (it & 1) * 128;
                 mb_wait(sm0 + oS + 8 * (it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, a.status);
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                uint32_t s[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32(ts + 32 * c, s[c]);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
                 const int left = a.T - (r.t0 + j) * kSharedTile;
-                if (left < kSharedTile) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                // 32 tokens at a time: the next ones are on their way out of tensor memory while these are worked on; P takes the place of
+                // scores that have been read
+                auto chunk = [&](int c, uint32_t (&s)[32], uint32_t (&next)[32]) {
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    if (c < 3) tmem_ld32(ts + 32 * (c + 1), next);
+                    if (left < kSharedTile) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (32 * c + i >= left) s[c][i] = 0xFF800000u;
-                }
-                float mx[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    mx[c] = __uint_as_float(s[c][0]);
-#pragma unroll
-                    for (int i = 1; i < 32; ++i) mx[c] = fmaxf(mx[c], __uint_as_float(s[c][i]));
-                }
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ks;
-                if (__any_sync(0xFFFFFFFFu, top > m + 8.f)) {  // (always at the first tile)
-                    const float m_new = fmaxf(m, top), f = ex2(m - m_new);
-                    if (j > 0) {
-                        mb_wait(sm0 + oO + 8 * ((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, abort_flag, a.status);
-                        __syncwarp();
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t o[32];
-                            tmem_ld32(tq + cO + 32 * c, o);
-                            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st32(tq + cO + 32 * c, o);
-                        }
-                        l *= f;
+                            if (i >= left - 32 * c) s[i] = 0xFF800000u;
                     }
-                    m = m_new;
-                }
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    float mx[4] = {__uint_as_float(s[0]), __uint_as_float(s[1]), __uint_as_float(s[2]), __uint_as_float(s[3])};
 #pragma unroll
-                for (int c = 0; c < 4; c += 2) {
-                    uint32_t p[32];
+                    for (int i = 4; i < 32; i += 8)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int k = 2 * i & 31;
-                        const float x = ex2(fmaf(__uint_as_float(s[c + (i >> 4)][k]), ks, -m)), y = ex2(fmaf(__uint_as_float(s[c + (i >> 4)][k + 1]), ks, -m));
-                        sum[(i & 1) * 2] += x;
-                        sum[(i & 1) * 2 + 1] += y;
+                        for (int k = 0; k < 4; ++k)
+                            mx[k] = i + 4 < 32 ? fmaxf(fmaxf(mx[k], __uint_as_float(s[i + k])), __uint_as_float(s[(i + 4 & 31) + k])) : fmaxf(mx[k], __uint_as_float(s[i + k]));
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ks;
+                    if (__any_sync(0xFFFFFFFFu, top > m + kLazy)) move_reference(top, j, c);
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float x, y;
+                        scaled2(s[2 * i], s[2 * i + 1], ks, -m, x, y);
+                        x = ex2(x);
+                        y = ex2(y);
+                        add2(sum[2 * (i & 1)], sum[2 * (i & 1) + 1], x, y);
                         p[i] = pack2(x, y);
                     }
-                    tmem_st32(ts + 16 * c, p);
+                    tmem_st16(ts + 16 * c, p);
+                };
+                uint32_t sa[32], sb[32];
+                tmem_ld32(ts, sa);
+#pragma unroll 1
+                for (int c = 0; c < 4; c += 2) {
+                    chunk(c, sa, sb);
+                    chunk(c + 1, sb, sa);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
@@ -430,7 +478,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             }
             if ((int)threadIdx.x < rows) {
                 part[(int64_t)sch.row_tile * 128 + threadIdx.x] = m * 0.6931471805599453f;  // the join works in natural-log units
-                part[(int64_t)sch.row_tile * 129 + threadIdx.x] = l;
+                part[(int64_t)sch.row_tile * 129 + threadIdx.x] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         }
@@ -441,7 +489,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    if (warp == 13) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
 }  // namespace
