@@ -215,20 +215,82 @@ struct SharedSeqs {
     int32_t slot[NB], len[NB];  // len counts this call's append
 };
 
+// Blocks [lo, hi] whose ranges meet item u.
+__device__ __forceinline__ void blocks_of_item(const SharedSched& sch, int u, int& lo, int& hi) {
+    lo = 0;
+    for (int step = 128; step; step >>= 1)
+        if (lo + step < sch.ncta && sch.start[lo + step] <= u * sch.tiles) lo += step;
+    hi = lo;
+    for (int step = 128; step; step >>= 1)
+        if (hi + step < sch.ncta && sch.start[hi + step] < (u + 1) * sch.tiles) hi += step;
+}
+
+// A softmax state: what the exponents are relative to (natural logarithm), their sum, four channels of the weighted sum.
+struct State4 {
+    float m = -INFINITY, l = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    __device__ __forceinline__ void add(float pm, float pl, const float4& o) {
+        const float mn = fmaxf(m, pm), ref = mn == -INFINITY ? 0.f : mn, f0 = __expf(m - ref), f1 = __expf(pm - ref);
+        l = l * f0 + pl * f1;
+        a.x = a.x * f0 + o.x * f1; a.y = a.y * f0 + o.y * f1; a.z = a.z * f0 + o.z * f1; a.w = a.w * f0 + o.w * f1;
+        m = mn;
+    }
+    // parts c, c + step, .. up to hi of the row r of an item (p0: its part of block 0), BATCH of them on their way at a time
+    template <int D, int BATCH>
+    __device__ __forceinline__ void add_parts(const float* p0, int64_t stride, int row_tile, int r, int c4, int c, int hi, int step) {
+        for (; c <= hi; c += BATCH * step) {
+            float pm[BATCH], pl[BATCH];
+            float4 po[BATCH];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const int cc = c + k * step;
+                const float* const part = p0 + (cc <= hi ? cc : c) * stride;
+                pm[k] = cc <= hi ? __ldcg(part + (int64_t)row_tile * D + r) : -INFINITY;
+                pl[k] = __ldcg(part + (int64_t)row_tile * (D + 1) + r);
+                po[k] = __ldcg(reinterpret_cast<const float4*>(part + ((int64_t)c4 * row_tile + r) * 4));
+            }
+            float mn = m;
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) mn = fmaxf(mn, pm[k]);
+            const float ref = mn == -INFINITY ? 0.f : mn, f0 = __expf(m - ref);
+            l *= f0;
+            a.x *= f0; a.y *= f0; a.z *= f0; a.w *= f0;
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const float f = __expf(pm[k] - ref);
+                l = fmaf(pl[k], f, l);
+                a.x = fmaf(po[k].x, f, a.x); a.y = fmaf(po[k].y, f, a.y); a.z = fmaf(po[k].z, f, a.z); a.w = fmaf(po[k].w, f, a.w);
+            }
+            m = mn;
+        }
+    }
+    __device__ __forceinline__ void store(void* out, int out_dtype, int64_t at) const {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        if (out_dtype == FDKV_BF16) {
+            const __nv_bfloat162 x = __floats2bfloat162_rn(a.x * inv, a.y * inv), y = __floats2bfloat162_rn(a.z * inv, a.w * inv);
+            *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(out) + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+        } else {
+            *reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + at) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+        }
+    }
+};
+
 constexpr int kJoinWarps = 8;
 
-// grid (Hkv, batch).  D / 8 lanes share a tail token, eight channels each; every such lane group keeps a softmax state of its own,
+// Portable join.  grid (Hkv, batch).  D / 8 lanes share a tail token, eight channels each; every such lane group keeps a softmax state of its own,
 // joined through shared memory with the prompt's parts.  The tails, q and the new rows are read before the dependency wait: the
 // prompt kernel lets this one start only behind its own, when all they come from is complete.
 template <typename T, int D, int G, int NB>
 __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(SharedArgs a, const __grid_constant__ SharedSched sch, const __grid_constant__ SharedSeqs<NB> sq) {
     using ACC = typename std::conditional<sizeof(T) == 4, double, float>::type;
     constexpr int LPT = D / 8, TPI = 32 / LPT, U = sizeof(T) == 4 || G == 8 ? 2 : 4;
+    // outputs in fours; threads that share one, each with its share of the parts
+    constexpr int ITEMS = G * D / 4, WAYS = kJoinWarps * 32 / ITEMS;
+    static_assert(WAYS >= 1 && WAYS * ITEMS == kJoinWarps * 32, "one four of outputs per thread");
     __shared__ __align__(16) float s_acc[kJoinWarps][G][D];
     __shared__ float s_m[kJoinWarps][G], s_l[kJoinWarps][G];
-    constexpr int JW = kJoinWarps * 32 / (G * D / 4) > 1 ? kJoinWarps * 32 / (G * D / 4) - 1 : 1;
-    __shared__ float4 j_acc[JW][G * D / 4];
-    __shared__ float2 j_ml[JW][G * D / 4];
+    __shared__ float4 j_acc[WAYS][ITEMS];
+    __shared__ float2 j_ml[WAYS][ITEMS];
     const int h = blockIdx.x, b = blockIdx.y;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LPT, c0 = lane % LPT * 8;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -323,79 +385,255 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(SharedArgs
             if (lane == 0) { s_m[warp][g] = M; s_l[warp][g] = l[g]; }
         }
     }
-    // ---- the blocks whose ranges meet the item of the unit's rows (row tiles hold whole sequences) ----
-    const int row0 = b * G, u = h * sch.groups + row0 / sch.row_tile, r0 = row0 % sch.row_tile;
-    int c_lo = 0;
-    for (int step = 128; step; step >>= 1)
-        if (c_lo + step < sch.ncta && sch.start[c_lo + step] <= u * sch.tiles) c_lo += step;
-    int c_hi = c_lo;  // the last block that starts before the item's end
-    for (int step = 128; step; step >>= 1)
-        if (c_hi + step < sch.ncta && sch.start[c_hi + step] < (u + 1) * sch.tiles) c_hi += step;
+    const int row0 = b * G, u = h * sch.groups + row0 / sch.row_tile, r0 = row0 % sch.row_tile;  // (row tiles hold whole sequences)
+    int c_lo, c_hi;
+    blocks_of_item(sch, u, c_lo, c_hi);
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the prompt's parts
-    // ---- four channels of a head per thread, the parts spread over as many threads as there are: six at a time on their way ----
-    constexpr int ITEMS = G * D / 4, WAYS = kJoinWarps * 32 / ITEMS > 0 ? kJoinWarps * 32 / ITEMS : 1, BATCH = 6;
-    for (int i0 = 0; i0 < ITEMS * WAYS; i0 += kJoinWarps * 32) {
-        const int i = (i0 + (int)threadIdx.x) % ITEMS, way = (i0 + (int)threadIdx.x) / ITEMS, g = i % G, c4 = i / G;
-        float M = -INFINITY, L = 0.f;
-        float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (i0 + (int)threadIdx.x < ITEMS * WAYS) {
-            const int64_t stride = shared_part_floats(sch.row_tile, D);
-            const float* const p0 = a.partials + u * stride;
-            for (int c = c_lo + way; c <= c_hi; c += BATCH * WAYS) {
-                float pm[BATCH], pl[BATCH];
-                float4 po[BATCH];
+    const int i = threadIdx.x % ITEMS, way = threadIdx.x / ITEMS, g = i % G, c4 = i / G;
+    const int64_t stride = shared_part_floats(sch.row_tile, D);
+    State4 s;
+    s.add_parts<D, 6>(a.partials + u * stride, stride, sch.row_tile, r0 + g, c4, c_lo + way, c_hi, WAYS);
+    if constexpr (WAYS > 1) {
+        j_acc[way][i] = s.a;
+        j_ml[way][i] = make_float2(s.m, s.l);
+        __syncthreads();
+        if (way > 0) return;
 #pragma unroll
-                for (int k = 0; k < BATCH; ++k) {
-                    const int cc = c + k * WAYS;
-                    const float* const part = p0 + (cc <= c_hi ? cc : c) * stride;
-                    pm[k] = cc <= c_hi ? __ldcg(part + (int64_t)sch.row_tile * D + r0 + g) : -INFINITY;
-                    pl[k] = __ldcg(part + (int64_t)sch.row_tile * (D + 1) + r0 + g);
-                    po[k] = __ldcg(reinterpret_cast<const float4*>(part + ((int64_t)c4 * sch.row_tile + r0 + g) * 4));
-                }
-                float mn = M;
+        for (int w = 1; w < WAYS; ++w) s.add(j_ml[w][i].x, j_ml[w][i].y, j_acc[w][i]);
+    }
 #pragma unroll
-                for (int k = 0; k < BATCH; ++k) mn = fmaxf(mn, pm[k]);
-                const float ref = mn == -INFINITY ? 0.f : mn, f0 = __expf(M - ref);
-                L *= f0;
-                A.x *= f0; A.y *= f0; A.z *= f0; A.w *= f0;
+    for (int w = 0; w < kJoinWarps; ++w) s.add(s_m[w][g], s_l[w][g], *reinterpret_cast<const float4*>(&s_acc[w][g][c4 * 4]));
+    s.store(a.out, a.out_dtype, ((int64_t)b * a.Hq + h * G + g) * D + c4 * 4);
+}
+
+// ------------------------------------------------------------------------------------------------ the join for bf16, 128 channels
+constexpr int kTcWarps = 4;
+constexpr int kMaxJoin = 8;  // thread blocks of a cluster
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t a) {  // an 8 x 8 matrix of 16-bit elements held by the warp
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&x);
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t peer_addr(const void* p, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float4 peer_load4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 peer_load2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+
+// grid (blocks of a cluster, Hkv, batch).  The tail on mma.sync, fragments straight from memory, sixteen tokens per warp and step:
+//   S[token][head] = K q^T     the sums over channels are in an order of the fragments' own, the same for K and q, so that a lane's 16
+//                              bytes of a row are two steps' fragments
+//   O^T[channel][head] += V^T P^T   a lane has eight channels of four tokens; a product's rows are channels eight apart
+// Up to four heads per group fill columns 0-3, columns 4-7 carry the remainder of P's rounding to bf16; eight heads take a second
+// product for it, so that P acts with 16 bits.  Blocks of a cluster share a unit's tail and parts (small batches, long tails).
+template <int G, int NB>
+__global__ void __launch_bounds__(kTcWarps * 32, 3) shared_join_tc_kernel(SharedArgs a, const __grid_constant__ SharedSched sch, const __grid_constant__ SharedSeqs<NB> sq) {
+    constexpr int D = 128, ITEMS = G * D / 4, THREADS = kTcWarps * 32;
+    constexpr int WAYS = THREADS / ITEMS > 0 ? THREADS / ITEMS : 1, ROUNDS = ITEMS > THREADS ? ITEMS / THREADS : 1;
+    constexpr bool SPLIT = G <= 4;
+    __shared__ __align__(16) float s_acc[kTcWarps][G][D];
+    __shared__ float s_m[kTcWarps][G], s_l[kTcWarps][G];
+    __shared__ __align__(16) float4 j_acc[WAYS][ITEMS];  // (in clusters the block's state, in row 0)
+    __shared__ __align__(16) float2 j_ml[WAYS][ITEMS];
+    const int rank = blockIdx.x, ranks = gridDim.x, h = blockIdx.y, b = blockIdx.z;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int n = sq.len[b], slot = sq.slot[b];
+    const int64_t tail0 = ((int64_t)slot * a.Hkv + h) * a.tail_rows * D;
+    __nv_bfloat16* const tk = reinterpret_cast<__nv_bfloat16*>(a.tail_k) + tail0;
+    __nv_bfloat16* const tv = reinterpret_cast<__nv_bfloat16*>(a.tail_v) + tail0;
+    const int64_t new0 = ((int64_t)b * a.Hkv + h) * D;
+    const __nv_bfloat16* const kn = a.k_new ? reinterpret_cast<const __nv_bfloat16*>(a.k_new) + new0 : nullptr;
+    const __nv_bfloat16* const vn = a.k_new ? reinterpret_cast<const __nv_bfloat16*>(a.v_new) + new0 : nullptr;
+
+    const int row0 = b * G, u = h * sch.groups + row0 / sch.row_tile, r0 = row0 % sch.row_tile;  // (row tiles hold whole sequences)
+    int c_lo, c_hi;
+    blocks_of_item(sch, u, c_lo, c_hi);
+
+    float o[8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
-                for (int k = 0; k < BATCH; ++k) {
-                    const float f = __expf(pm[k] - ref);
-                    L = fmaf(pl[k], f, L);
-                    A.x = fmaf(po[k].x, f, A.x); A.y = fmaf(po[k].y, f, A.y); A.z = fmaf(po[k].z, f, A.z); A.w = fmaf(po[k].w, f, A.w);
-                }
-                M = mn;
+    for (int j = 0; j < 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+    const int first = (rank * kTcWarps + warp) * 16, step = ranks * kTcWarps * 16;
+    if (first < n) {
+        const int qcol = SPLIT ? gid & 3 : gid;
+        uint4 q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            q[k] = qcol < G ? __ldcg(reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + ((int64_t)b * a.Hq + h * G + qcol) * D + 32 * k + 8 * tig))
+                            : make_uint4(0u, 0u, 0u, 0u);
+        const float ks = 0.08838834764831845f * 1.4426950408889634f;  // / sqrt(128), in powers of two
+#pragma unroll 1
+        for (int t0 = first; t0 < n; t0 += step) {
+            // (rows behind the last are read as the last and masked; the appended one comes from the caller)
+            uint4 k[2][4], v[4][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int t = min(t0 + gid + 8 * i, n - 1);
+                const __nv_bfloat16* const p = (kn && t == n - 1 ? kn : tk + (int64_t)t * D) + 8 * tig;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) k[i][c] = __ldcg(reinterpret_cast<const uint4*>(p + 32 * c));
             }
-        }
-        auto add = [&](float pm, float pl, const float4& o) {
-            const float mn = fmaxf(M, pm), ref = mn == -INFINITY ? 0.f : mn, f0 = __expf(M - ref), f1 = __expf(pm - ref);
-            L = L * f0 + pl * f1;
-            A.x = A.x * f0 + o.x * f1; A.y = A.y * f0 + o.y * f1; A.z = A.z * f0 + o.z * f1; A.w = A.w * f0 + o.w * f1;
-            M = mn;
-        };
-        if constexpr (WAYS > 1) {  // (one round: every thread has at most one item)
-            if (way > 0 && way < WAYS) {
-                j_acc[way - 1][i] = A;
-                j_ml[way - 1][i] = make_float2(M, L);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = min(t0 + 2 * tig + (i & 1) + 8 * (i >> 1), n - 1);
+                const __nv_bfloat16* const p = (kn && t == n - 1 ? vn : tv + (int64_t)t * D) + 8 * gid;
+                v[i][0] = __ldcg(reinterpret_cast<const uint4*>(p));
+                v[i][1] = __ldcg(reinterpret_cast<const uint4*>(p + 64));
             }
-            __syncthreads();
-            if (way > 0) return;
+            float s[2][4] = {};
 #pragma unroll
-            for (int w = 1; w < WAYS; ++w) add(j_ml[w - 1][i].x, j_ml[w - 1][i].y, j_acc[w - 1][i]);
-        }
-        if (i0 + (int)threadIdx.x >= ITEMS * WAYS) return;
+            for (int c = 0; c < 4; ++c) {
+                mma_bf16(s[0], k[0][c].x, k[1][c].x, k[0][c].y, k[1][c].y, q[c].x, q[c].y);
+                mma_bf16(s[1], k[0][c].z, k[1][c].z, k[0][c].w, k[1][c].w, q[c].z, q[c].w);
+            }
+            float p[2][2], mt[2];
 #pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) add(s_m[w][g], s_l[w][g], *reinterpret_cast<const float4*>(&s_acc[w][g][c4 * 4]));
-        const float inv = L > 0.f ? 1.f / L : 0.f;
-        const int64_t o = ((int64_t)b * a.Hq + h * G + g) * D + c4 * 4;
-        if (a.out_dtype == FDKV_BF16) {
-            const __nv_bfloat162 x = __floats2bfloat162_rn(A.x * inv, A.y * inv), y = __floats2bfloat162_rn(A.z * inv, A.w * inv);
-            *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + o) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-        } else {
-            *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + o) = make_float4(A.x * inv, A.y * inv, A.z * inv, A.w * inv);
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) p[i][e] = t0 + gid + 8 * i < n ? (s[0][2 * i + e] + s[1][2 * i + e]) * ks : -INFINITY;
+                mt[e] = fmaxf(p[0][e], p[1][e]);
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) mt[e] = fmaxf(mt[e], __shfl_xor_sync(0xFFFFFFFFu, mt[e], x));
+                const float mn = fmaxf(m[e], mt[e]), f = ex2(m[e] - mn);  // (finite: every step has a token)
+                m[e] = mn;
+                l[e] *= f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { o[j][e] *= f; o[j][2 + e] *= f; }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    p[i][e] = ex2(p[i][e] - mn);
+                    l[e] += p[i][e];
+                }
+            }
+            uint32_t ph[2], pl[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float h0 = __bfloat162float(__float2bfloat16_rn(p[i][0])), h1 = __bfloat162float(__float2bfloat16_rn(p[i][1]));
+                const uint32_t lo = pack2(p[i][0] - h0, p[i][1] - h1), hi = pack2(h0, h1);
+                ph[i] = transposed(SPLIT && tig >= 2 ? lo : hi);
+                if constexpr (!SPLIT) pl[i] = transposed(lo);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint32_t x[4][2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) x[i][c] = j < 2 ? v[i][c].x : j < 4 ? v[i][c].y : j < 6 ? v[i][c].z : v[i][c].w;
+                const uint32_t sel = j & 1 ? 0x7632 : 0x5410;
+                const uint32_t a0 = __byte_perm(x[0][0], x[1][0], sel), a1 = __byte_perm(x[0][1], x[1][1], sel), a2 = __byte_perm(x[2][0], x[3][0], sel),
+                               a3 = __byte_perm(x[2][1], x[3][1], sel);
+                mma_bf16(o[j], a0, a1, a2, a3, ph[0], ph[1]);
+                if constexpr (!SPLIT) mma_bf16(o[j], a0, a1, a2, a3, pl[0], pl[1]);
+            }
         }
     }
+    if (kn && rank == 0 && warp == 0) {  // the new row joins the tail for later calls: lanes 0-15 K, lanes 16-31 V
+        const int c = lane & 15;
+        reinterpret_cast<uint4*>((lane < 16 ? tk : tv) + (int64_t)(n - 1) * D)[c] = __ldcg(reinterpret_cast<const uint4*>(lane < 16 ? kn : vn) + c);
+        if (lane == 0 && h == 0) a.tail_len[slot] = n;
+    }
+    // ---- the warps' states: lane (gid, tig) has channels 8 gid .. and 64 + 8 gid .. of columns 2 tig and 2 tig + 1 ----
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], x);
+        float w[16];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            w[j] = o[j][e];
+            w[8 + j] = o[j][2 + e];
+            if (SPLIT) {
+                w[j] += __shfl_xor_sync(0xFFFFFFFFu, w[j], 2);
+                w[8 + j] += __shfl_xor_sync(0xFFFFFFFFu, w[8 + j], 2);
+            }
+        }
+        const int g = 2 * tig + e;
+        if (g < G) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(&s_acc[warp][g][(j >> 3) * 64 + 8 * gid + (j & 7)]) = make_float4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+            if (gid == 0) {
+                s_m[warp][g] = m[e] * 0.6931471805599453f;  // natural logarithms from here on
+                s_l[warp][g] = l[e];
+            }
+        }
+    }
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the prompt's parts
+    const int64_t stride = shared_part_floats(sch.row_tile, D);
+    const float* const p0 = a.partials + u * stride;
+#pragma unroll
+    for (int round = 0; round < ROUNDS; ++round) {
+        const int i = (int)threadIdx.x % ITEMS + round * THREADS, way = threadIdx.x / ITEMS, g = i % G, c4 = i / G;
+        State4 s;
+        s.add_parts<D, 6>(p0, stride, sch.row_tile, r0 + g, c4, c_lo + rank + way * ranks, c_hi, WAYS * ranks);
+        if constexpr (WAYS > 1) {
+            j_acc[way][i] = s.a;
+            j_ml[way][i] = make_float2(s.m, s.l);
+            __syncthreads();
+            if (way == 0)
+#pragma unroll
+                for (int w = 1; w < WAYS; ++w) s.add(j_ml[w][i].x, j_ml[w][i].y, j_acc[w][i]);
+        }
+        if (way == 0) {
+#pragma unroll
+            for (int w = 0; w < kTcWarps; ++w) s.add(s_m[w][g], s_l[w][g], *reinterpret_cast<const float4*>(&s_acc[w][g][c4 * 4]));
+            if (ranks == 1) {
+                s.store(a.out, a.out_dtype, ((int64_t)b * a.Hq + h * G + g) * D + c4 * 4);
+            } else {
+                j_acc[0][i] = s.a;
+                j_ml[0][i] = make_float2(s.m, s.l);
+            }
+        }
+    }
+    if (ranks == 1) return;
+    // ---- the cluster's blocks: each joins and writes its share of the outputs ----
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    const int share = ITEMS / ranks;
+    for (int k = threadIdx.x; k < share; k += THREADS) {
+        const int i = rank * share + k;
+        float4 pa[kMaxJoin];
+        float2 pm[kMaxJoin];
+#pragma unroll
+        for (int c = 0; c < kMaxJoin; ++c)
+            if (c < ranks) {
+                pa[c] = peer_load4(peer_addr(&j_acc[0][i], c));
+                pm[c] = peer_load2(peer_addr(&j_ml[0][i], c));
+            }
+        State4 s;
+#pragma unroll
+        for (int c = 0; c < kMaxJoin; ++c)
+            if (c < ranks) s.add(pm[c].x, pm[c].y, pa[c]);
+        s.store(a.out, a.out_dtype, ((int64_t)b * a.Hq + h * G + i % G) * D + i / G * 4);
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");  // (the peers have read this block's state)
 }
 
 cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t st, cudaLaunchAttribute* attr) {
@@ -411,15 +649,20 @@ cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t st, 
     return cfg;
 }
 
-template <typename T, int D, int NB>
-cudaError_t launch_join(const SharedArgs& a, const SharedSched& sch, cudaStream_t st) {
-    cudaLaunchAttribute attr[1];
-    cudaLaunchConfig_t cfg = config(dim3(a.Hkv, a.batch), kJoinWarps * 32, 0, st, attr);
+template <int NB>
+SharedSeqs<NB> seqs_of(const SharedArgs& a) {
     SharedSeqs<NB> sq;
     for (int b = 0; b < a.batch; ++b) {
         sq.slot[b] = a.seqs[b];
         sq.len[b] = a.lens[b];
     }
+    return sq;
+}
+template <typename T, int D, int NB>
+cudaError_t launch_join(const SharedArgs& a, const SharedSched& sch, cudaStream_t st) {
+    cudaLaunchAttribute attr[1];
+    cudaLaunchConfig_t cfg = config(dim3(a.Hkv, a.batch), kJoinWarps * 32, 0, st, attr);
+    const SharedSeqs<NB> sq = seqs_of<NB>(a);
     switch (a.G) {
         case 1: return cudaLaunchKernelEx(&cfg, shared_join_kernel<T, D, 1, NB>, a, sch, sq);
         case 2: return cudaLaunchKernelEx(&cfg, shared_join_kernel<T, D, 2, NB>, a, sch, sq);
@@ -431,6 +674,29 @@ cudaError_t launch_join(const SharedArgs& a, const SharedSched& sch, cudaStream_
 template <typename T, int D>
 cudaError_t launch_join(const SharedArgs& a, const SharedSched& sch, cudaStream_t st) {
     return a.batch <= kSharedFew ? launch_join<T, D, kSharedFew>(a, sch, st) : launch_join<T, D, kMaxShared>(a, sch, st);
+}
+template <int NB>
+cudaError_t launch_join_tc(const SharedArgs& a, const SharedSched& sch, int sms, cudaStream_t st) {
+    // blocks per unit: more than one while they leave half of the device idle and have parts or tail tokens for each
+    int longest = 0;
+    for (int b = 0; b < a.batch; ++b) longest = std::max(longest, a.lens[b]);
+    const int parts = std::max(1, sch.ncta / (a.Hkv * sch.groups));
+    int ranks = 1;
+    while (ranks < kMaxJoin && a.Hkv * a.batch * ranks <= sms && (parts >= 8 * ranks || longest >= 128 * ranks)) ranks *= 2;
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = config(dim3(ranks, a.Hkv, a.batch), kTcWarps * 32, 0, st, attr);
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ranks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = ranks > 1 ? 2 : 1;
+    const SharedSeqs<NB> sq = seqs_of<NB>(a);
+    switch (a.G) {
+        case 1: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<1, NB>, a, sch, sq);
+        case 2: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<2, NB>, a, sch, sq);
+        case 4: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<4, NB>, a, sch, sq);
+        case 8: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<8, NB>, a, sch, sq);
+        default: return cudaErrorInvalidValue;
+    }
 }
 
 template <typename T, int D>
@@ -469,7 +735,7 @@ cudaError_t launch_shared_decode(const SharedArgs& a, int dtype, cudaStream_t st
     if ((e = plan_shared(a, tc ? 128 : kRows, sms, sch)) != cudaSuccess) return e;
     if (tc) {
         e = launch_shared_tc(a, sch, st);
-        if (e == cudaSuccess) e = launch_join<__nv_bfloat16, 128>(a, sch, st);
+        if (e == cudaSuccess) e = a.batch <= kSharedFew ? launch_join_tc<kSharedFew>(a, sch, sms, st) : launch_join_tc<kMaxShared>(a, sch, sms, st);
     } else if (dtype == FDKV_BF16) {
         if (a.d == 128) return cudaErrorNotSupported;  // (no tensor map of the arena)
         e = launch_part<__nv_bfloat16, 64>(a, sch, st);
