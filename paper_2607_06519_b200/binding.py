@@ -209,17 +209,21 @@ class Rotary:
         self._inv = (C.c_float * max(m, 1))(*[float(f) for f in inv_freq])
         self._axis = None if axis_of is None else (C.c_int32 * max(m, 1))(*[int(a) for a in axis_of])
         self.n_axes, self.q_weight, self.k_weight = n_axes, q_weight, k_weight
+        self._rows = None  # what the struct's sizes were set for
         self._c = _Rotary(1, 1, 0, 0, 2 * m, int(interleaved), n_axes, eps, scale, C.addressof(self._inv),
                           None if self._axis is None else C.addressof(self._axis),
                           None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
 
     def c(self, n_q_heads: int, n_kv_heads: int, head_dim: int, tdtype) -> _Rotary:
-        for w in (self.q_weight, self.k_weight):
-            if w is not None and (w.dtype is not tdtype or len(w) != head_dim):
-                raise ValueError("norm weights must have the rows' dtype and head_dim")
-        r = self._c
-        r.n_q_heads, r.n_kv_heads, r.head_dim, r.dtype = n_q_heads, n_kv_heads, head_dim, _dtype_code(tdtype)
-        return r
+        rows = (n_q_heads, n_kv_heads, head_dim, tdtype)
+        if rows != self._rows:
+            for w in (self.q_weight, self.k_weight):
+                if w is not None and (w.dtype is not tdtype or len(w) != head_dim):
+                    raise ValueError("norm weights must have the rows' dtype and head_dim")
+            r = self._c
+            r.n_q_heads, r.n_kv_heads, r.head_dim, r.dtype = n_q_heads, n_kv_heads, head_dim, _dtype_code(tdtype)
+            self._rows = rows
+        return self._c
 
 
 def _dtype_code(tdtype) -> int:
@@ -232,9 +236,10 @@ def _dtype_code(tdtype) -> int:
 
 def _positions(positions, n_axes: int, n: int) -> int:
     """The distance between the axes of positions [n_axes, n], or [n] for one axis."""
-    if positions.dtype is not torch.int32 or tuple(positions.shape) not in ((n_axes, n),) + (((n,),) if n_axes == 1 else ()) or (n > 1 and positions.stride(-1) != 1):
+    shape, strides = tuple(positions.shape), positions.stride()
+    if positions.dtype is not torch.int32 or (shape != (n_axes, n) and not (n_axes == 1 and shape == (n,))) or (n > 1 and strides[-1] != 1):
         raise ValueError("positions must be int32 [n_axes, n], dense along n")
-    return positions.stride(0) if positions.dim() == 2 and n_axes > 1 else n
+    return strides[0] if n_axes > 1 else n
 
 
 def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream=None):
@@ -242,25 +247,38 @@ def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream
     Tensors may be strided (a slice of the fused projection, a layer's rows); an output may be its own input."""
     x = q if q is not None else k
     n, _, d = x.shape
-    if q_out is None and q is not None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k_out is None and k is not None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    args = []
-    for t, like in ((q, q), (k, k), (q_out, q), (k_out, k)):
-        if t is None:
-            args.append((None, 0, 0))
-            continue
-        st, sh, sc = t.stride()
-        if sc != 1 or t.dtype is not x.dtype or t.shape != like.shape or t.shape[0] != n or t.shape[2] != d:
-            raise ValueError("queries and keys must be [n, heads, d] of one dtype, dense along d")
-        args.append((t.data_ptr(), st if n > 1 else d, sh if t.shape[1] > 1 else d))
+    dtype = x.dtype
+    q_args = q_to = k_args = k_to = _NO_ROWS
+    hq = hk = 1
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        hq, q_args, q_to = q.shape[1], _rows(q, n, d, dtype), _rows(q_out, n, d, dtype)
+        if q_out.shape[1] != hq:
+            raise ValueError("q_out must have the shape of q")
+    if k is not None:
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
+        hk, k_args, k_to = k.shape[1], _rows(k, n, d, dtype), _rows(k_out, n, d, dtype)
+        if k_out.shape[1] != hk:
+            raise ValueError("k_out must have the shape of k")
     step = _positions(positions, rotary.n_axes, n) if positions is not None else 0
-    c = rotary.c(q.shape[1] if q is not None else 1, k.shape[1] if k is not None else 1, d, x.dtype)
-    st = _qk_norm_rope(c, n, *args[0], *args[1], None if positions is None else positions.data_ptr(), step, *args[2], *args[3], _stream(stream))
+    st = _qk_norm_rope(rotary.c(hq, hk, d, dtype), n, *q_args, *k_args, None if positions is None else positions.data_ptr(), step, *q_to, *k_to, _stream(stream))
     if st:
         raise FdkvError(st, "fdkv_qk_norm_rope")
     return q_out, k_out
+
+
+_NO_ROWS = (None, 0, 0)
+
+
+def _rows(t, n: int, d: int, dtype):
+    """Address and strides (token, head) of rows [n, heads, d]; a stride that nothing is reached by counts as d."""
+    tn, th, td = t.shape
+    st, sh, sc = t.stride()
+    if sc != 1 or tn != n or td != d or t.dtype is not dtype:
+        raise ValueError("queries and keys must be [n, heads, d] of one dtype, dense along d")
+    return t.data_ptr(), st if n > 1 else d, sh if th > 1 else d
 
 
 def _slots(seqs):
