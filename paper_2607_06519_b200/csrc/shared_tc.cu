@@ -11,7 +11,10 @@
 //              running maximum only moves, and O is only rescaled, where a score passes it by more than 2^16
 // All tiles, rows and entries alike, go through one ring of 32 KiB slots in the order in which the products use them: K of the next
 // tile lies before V of this one, so that the next S is formed while the softmax of this one runs (S has two accumulators).
-// P in bf16: a probability is off by 2^-8 at most, each its own way; the sums l are those of the unrounded ones.
+// P in bf16: a probability is off by 2^-8 at most, each its own way.  Its sum is that of the rounded ones, a third product with a column
+// of ones: what is wrong with a probability then shifts the mean instead of scaling it (a row with one large probability is not
+// off at all), and the softmax has no additions to do.  (Sums of the unrounded ones: outputs off by 2.3e-3 instead of 1.7e-3, of which 1.7e-3 is the
+// rounding of the outputs.)
 #include <cuda.h>
 
 #include "fdkv_internal.h"
@@ -24,14 +27,15 @@ namespace {
 constexpr int kThreads = 448;
 constexpr int kSlots = 7, kSlotBytes = 32768, kHalf = 16384;
 constexpr float kLazy = 16.f;  // (powers of two)
-constexpr int kHeader = 1024;
-constexpr int kSmem = kHeader + kSlots * kSlotBytes;
+constexpr int kHeader = 1024, kOnes = 2048;  // (16 rows of 128 bytes, bf16 ones)
+constexpr int kSmem = kHeader + kOnes + kSlots * kSlotBytes;
 static_assert(kSmem <= 227 * 1024, "shared memory budget");
 // header
 constexpr int oFull = 0, oEmpty = 64, oS = 128, oP = 144, oO = 160, oQ = 176, oAbort = 184, oTmem = 188, oRun = 192;
 // tensor memory columns
-constexpr uint32_t cS = 0, cO = 256, cQ = 384;
+constexpr uint32_t cS = 0, cO = 256, cQ = 384, cL = 448;
 constexpr uint32_t kIdescS = umma_idesc(128, 128, false), kIdescO = umma_idesc(128, 128, false) | (1u << 16);  // (B of the second product is MN-major)
+constexpr uint32_t kIdescL = umma_idesc(128, 16, false);
 
 // D[tmem] (+)= A[tmem] * B[smem]
 template <uint32_t IDESC>
@@ -76,9 +80,6 @@ __device__ __forceinline__ void scaled2(uint32_t a, uint32_t b, float s, float t
         : "=f"(x), "=f"(y)
         : "r"(a), "r"(b), "f"(s), "f"(t));
 }
-__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
-    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tadd.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
-}
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
@@ -117,7 +118,7 @@ __device__ __forceinline__ bool next_run(const SharedSched& sch, int& g, int g_e
 __global__ void __launch_bounds__(kThreads, 1)
 shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const __grid_constant__ SharedSched sch) {
     extern __shared__ __align__(1024) uint8_t smem[];
-    const uint32_t sm0 = s_u32(smem), slot0 = sm0 + kHeader;
+    const uint32_t sm0 = s_u32(smem), ones = sm0 + kHeader, slot0 = ones + kOnes;
     volatile uint32_t* const abort_flag = reinterpret_cast<volatile uint32_t*>(smem + oAbort);
     volatile uint32_t* const run_no = reinterpret_cast<volatile uint32_t*>(smem + oRun);  // runs that the producer has begun
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (uniform to the compiler)
@@ -140,6 +141,10 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
         *abort_flag = 0;
         *run_no = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x < kOnes / 16) {
+        st_v4(ones + threadIdx.x * 16, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 13) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sm0 + oTmem), "r"(512u) : "memory");
@@ -191,6 +196,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             // The whole warp walks the loop and one lane issues, so that descriptors and addresses stay in uniform registers: with
             // the loop behind `if (lane == 0)` issuing a tile's products took 2 700 cycles, more than the softmax.
             const bool leader = elect_one();
+            const uint64_t one = smem_desc(ones);
             int it = 0;
             uint32_t qph = 0;
             bool ok = true;
@@ -227,6 +233,9 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                         if (leader && ok) {
 #pragma unroll
                             for (int k = 0; k < 8; ++k) umma_ts<kIdescO>(tmem + cO, tp + 8 * k, d + k * (2048 >> 4), j > 0 || e > 0 || k > 0);
+                            if (e == 0)
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) umma_ts<kIdescL>(tmem + cL, tp + 8 * k, one, j > 0 || k > 0);
                             umma_commit(sm0 + oEmpty + 8 * sl);
                             if (e + 1 == parts) umma_commit(sm0 + oO + 8 * (it & 1));
                         }
@@ -378,16 +387,15 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 if (lane == 0) mb_arrive(sm0 + oQ);
             }
             float m = -INFINITY;                    // what the exponents are relative to, in powers of two
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-            // A score passes the reference by more than 2^kLazy (or there is none yet): the row's sums, its accumulators and what this tile
+            // A score passes the reference by more than 2^kLazy (or there is none yet): the row's accumulators and what this tile
             // has of its P are scaled down, by a power of two, so that P stays exactly as it was rounded.
             auto move_reference = [&](float top, int j, int c) {
-                const float m_new = fmaxf(m, ceilf(top));
-                const float f = ex2(m - m_new);  // (0 at the first scores)
-                m = m_new;
-                if (j == 0 && c == 0) return;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i] *= f;
+                if (j == 0 && c == 0) {
+                    m = top;
+                    return;
+                }
+                const float up = fmaxf(0.f, ceilf(top - m)), f = ex2(-up);
+                m += up;
                 const uint32_t tp = tq + cS + (it & 1) * 128;
 #pragma unroll 1
                 for (int k = 0; k < c; ++k) {
@@ -411,6 +419,11 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                     for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
                     tmem_st16(tq + cO + 16 * k, o);
                 }
+                uint32_t o[16];
+                tmem_ld16(tq + cL, o);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                o[0] = __float_as_uint(__uint_as_float(o[0]) * f);
+                tmem_st16(tq + cL, o);
             };
             for (int j = 0; j < r.n; ++j, ++it) {
                 const uint32_t ts = tq + cS + (it & 1) * 128;
@@ -443,7 +456,6 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                         scaled2(s[2 * i], s[2 * i + 1], ks, -m, x, y);
                         x = ex2(x);
                         y = ex2(y);
-                        add2(sum[2 * (i & 1)], sum[2 * (i & 1) + 1], x, y);
                         p[i] = pack2(x, y);
                     }
                     tmem_st16(ts + 16 * c, p);
@@ -476,9 +488,12 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                             make_float4(__uint_as_float(o[4 * i]) * uscale, __uint_as_float(o[4 * i + 1]) * uscale, __uint_as_float(o[4 * i + 2]) * uscale,
                                         __uint_as_float(o[4 * i + 3]) * uscale);
             }
+            uint32_t sum[16];
+            tmem_ld16(tq + cL, sum);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
             if ((int)threadIdx.x < rows) {
                 part[(int64_t)sch.row_tile * 128 + threadIdx.x] = m * 0.6931471805599453f;  // the join works in natural-log units
-                part[(int64_t)sch.row_tile * 129 + threadIdx.x] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                part[(int64_t)sch.row_tile * 129 + threadIdx.x] = __uint_as_float(sum[0]);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         }
