@@ -2,13 +2,14 @@
 // sequences of a KV head fill the rows of tcgen05 products, so that a tile of the compressed prompt is read once and used by up to 128 rows.
 //
 // A persistent block per SM walks a range of the flat (KV head, row group, 128-token tile) list:
-//   warp 12    TMA producer: the tile's K and V rows (2 x 64 channels x 128 tokens, 128-byte swizzle)
-//   warps 4-11 residual units: the tile's kept entries of K (4-7) and V (8-11), scattered into a zeroed tile of the same layout (32
+//   warp 16    TMA producer: the tile's K and V rows (2 x 64 channels x 128 tokens, 128-byte swizzle)
+//   warps 8-15 residual units: the tile's kept entries of K (8-11) and V (12-15), scattered into a zeroed tile of the same layout (32
 //              tokens per warp)
-//   warp 13    issues S = Q K^T (Q from tensor memory, K-major K) and O += P V (P from tensor memory, MN-major V).  Residual units add
+//   warp 17    issues S = Q K^T (Q from tensor memory, K-major K) and O += P V (P from tensor memory, MN-major V).  Residual units add
 //              the products with the entries' tiles into the same accumulators, so that the correction is exact in float32
-//   warps 0-3  softmax: thread = query row.  S is read from tensor memory, P = exp2(S - max) rounded to bf16 takes its place; the
-//              running maximum only moves, and O is only rescaled, where a score passes it by more than 2^16
+//   warps 0-7  softmax: thread = query row and half of the tile's tokens.  S is read from tensor memory, P = exp2(S - m) rounded to bf16
+//              takes its place; the reference m only moves, and O is only rescaled, where a score passes it by more than 2^16.  (One
+//              warp per scheduler, four in all, took 2 900 cycles for a tile, its chains of maxima and exponentials in the open.)
 // All tiles, rows and entries alike, go through one ring of 32 KiB slots in the order in which the products use them: K of the next
 // tile lies before V of this one, so that the next S is formed while the softmax of this one runs (S has two accumulators).
 // P in bf16: a probability is off by 2^-8 at most, each its own way.  Its sum is that of the rounded ones, a third product with a column
@@ -24,7 +25,7 @@ namespace fdkv {
 
 namespace {
 
-constexpr int kThreads = 448;
+constexpr int kThreads = 640;  // five warpgroups; the last one's warps 18 and 19 have nothing to do
 constexpr int kSlots = 7, kSlotBytes = 32768, kHalf = 16384;
 constexpr float kLazy = 16.f;  // (powers of two)
 constexpr int kHeader = 1024, kOnes = 2048;  // (16 rows of 128 bytes, bf16 ones)
@@ -33,7 +34,7 @@ static_assert(kSmem <= 227 * 1024, "shared memory budget");
 // header
 constexpr int oFull = 0, oEmpty = 64, oS = 128, oP = 144, oO = 160, oQ = 176, oAbort = 184, oTmem = 188, oRun = 192;
 // tensor memory columns
-constexpr uint32_t cS = 0, cO = 256, cQ = 384, cL = 448;
+constexpr uint32_t cS = 0, cO = 256, cQ = 384, cL = 448, cX = 464;
 constexpr uint32_t kIdescS = umma_idesc(128, 128, false), kIdescO = umma_idesc(128, 128, false) | (1u << 16);  // (B of the second product is MN-major)
 constexpr uint32_t kIdescL = umma_idesc(128, 16, false);
 
@@ -91,6 +92,19 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
                  "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
+__device__ __forceinline__ uint32_t tmem_ld1(uint32_t taddr) {
+    uint32_t x;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(x) : "r"(taddr) : "memory");
+    return x;
+}
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, uint32_t x) { asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(x) : "memory"); }
+// the two warps of a pair (hardware barriers 1 to 4): whether some thread's x holds; or only meet
+__device__ __forceinline__ bool pair_any(int pair, bool x) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %2, 0;\n\tbarrier.cta.red.or.pred p, %1, 64, q;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r) : "r"(pair + 1), "r"((uint32_t)x) : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ void pair_sync(int pair) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair + 1) : "memory"); }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -115,6 +129,7 @@ __device__ __forceinline__ bool next_run(const SharedSched& sch, int& g, int g_e
     return true;
 }
 
+// 640 threads x 96 registers at launch; the softmax's two warpgroups take 128, the others keep 72 (together 472 of the 480 per thread of a warpgroup).
 __global__ void __launch_bounds__(kThreads, 1)
 shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const __grid_constant__ SharedSched sch) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -133,11 +148,11 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
         }
         for (int i = 0; i < 2; ++i) {
             mb_init(sm0 + oS + 8 * i, 1);
-            mb_init(sm0 + oP + 8 * i, 4);
+            mb_init(sm0 + oP + 8 * i, 8);
             // (two: the S that a warp has seen says that the product with P two tiles back is done, not the one before)
             mb_init(sm0 + oO + 8 * i, 1);
         }
-        mb_init(sm0 + oQ, 4);
+        mb_init(sm0 + oQ, 8);
         *abort_flag = 0;
         *run_no = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -146,7 +161,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
         st_v4(ones + threadIdx.x * 16, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == 13) {
+    if (warp == 17) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sm0 + oTmem), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -164,8 +179,9 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
         if (++sl == kSlots) { sl = 0; ph ^= 1u; }
     };
 
-    if (warp >= 12) {
-        if (warp == 12) {
+    if (warp >= 16) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 16) {
             if (lane == 0) {
                 uint32_t runs = 0;
                 while (next_run(sch, g, g_end, r)) {
@@ -192,7 +208,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                     }
                 }
             }
-        } else if (warp == 13) {
+        } else if (warp == 17) {
             // The whole warp walks the loop and one lane issues, so that descriptors and addresses stay in uniform registers: with
             // the loop behind `if (lane == 0)` issuing a tile's products took 2 700 cycles, more than the softmax.
             const bool leader = elect_one();
@@ -245,10 +261,11 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 }
             }
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 8) {
         // ---- the residual's tiles of K or of V: this warp has tokens [32 w, 32 w + 32) of them, two 16-token slices ----
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         const int w = warp & 3;
-        const bool is_v = warp >= 8;
+        const bool is_v = warp >= 12;
         uint32_t runs = 0;
         while (next_run(sch, g, g_end, r)) {
             const UnitDesc ud = a.desc[r.h];
@@ -360,7 +377,9 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
         }
     } else {
         // ---- softmax: thread = query row = tensor memory lane ----
-        const uint32_t tq = tmem + ((uint32_t)(warp * 32) << 16);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+        const int pair = warp & 3, half = warp >> 2, row = pair * 32 + lane;
+        const uint32_t tq = tmem + ((uint32_t)(pair * 32) << 16);
         asm volatile("griddepcontrol.wait;" ::: "memory");  // q and the parts belong to the kernels ahead
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (behind the wait: the join reads the tails before its own)
         int it = 0;
@@ -369,104 +388,92 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             const float uscale = a.desc[r.h].scale;
             const float ks = uscale * (0.08838834764831845f * 1.4426950408889634f);  // / sqrt(128), in powers of two
             {
-                const int row = r.row0 + (int)threadIdx.x, b = row / a.G;
-                const char* const src = reinterpret_cast<const char*>(a.q) + (((int64_t)b * a.Hq + r.h * a.G + (row - b * a.G)) << 8);
-                uint32_t x[2][32];
+                const int i = r.row0 + row, b = i / a.G;
+                const char* const src = reinterpret_cast<const char*>(a.q) + (((int64_t)b * a.Hq + r.h * a.G + (i - b * a.G)) << 8) + 128 * half;
+                uint32_t x[32];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if ((int)threadIdx.x < rows) ldcg32(src + 32 * i, &x[i >> 2][8 * (i & 3)]);
+                for (int k = 0; k < 4; ++k) {
+                    if (row < rows) ldcg32(src + 32 * k, &x[8 * k]);
                     else
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) x[i >> 2][8 * (i & 3) + k] = 0u;
+                        for (int e = 0; e < 8; ++e) x[8 * k + e] = 0u;
                 }
-                tmem_st32(tq + cQ, x[0]);
-                tmem_st32(tq + cQ + 32, x[1]);
+                tmem_st32(tq + cQ + 32 * half, x);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mb_arrive(sm0 + oQ);
             }
-            float m = -INFINITY;                    // what the exponents are relative to, in powers of two
-            // A score passes the reference by more than 2^kLazy (or there is none yet): the row's accumulators and what this tile
-            // has of its P are scaled down, by a power of two, so that P stays exactly as it was rounded.
-            auto move_reference = [&](float top, int j, int c) {
-                if (j == 0 && c == 0) {
+            float m = -INFINITY;  // what the exponents are relative to, in powers of two: the same for both halves
+            // A score of the warps' rows passes the reference by more than 2^kLazy (or there is none yet): both halves take the larger of their
+            // maxima, and each scales its half of the accumulators down, by a power of two.
+            auto move_reference = [&](float top, int j) {
+                tmem_st1(tq + cX + half, __float_as_uint(top));
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                pair_sync(pair);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                top = fmaxf(top, __uint_as_float(tmem_ld1(tq + cX + (half ^ 1))));
+                // (the other half has read this one's before either comes here again: the barrier of the next tile lies between)
+                if (j == 0) {
                     m = top;
                     return;
                 }
                 const float up = fmaxf(0.f, ceilf(top - m)), f = ex2(-up);
                 m += up;
-                const uint32_t tp = tq + cS + (it & 1) * 128;
-#pragma unroll 1
-                for (int k = 0; k < c; ++k) {
-                    uint32_t x[16];
-                    tmem_ld16(tp + 16 * k, x);
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = pack2(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xFFFF0000u) * f);
-                    tmem_st16(tp + 16 * k, x);
-                }
-                if (j == 0) return;
                 mb_wait(sm0 + oO + 8 * ((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, abort_flag, a.status);
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
-                for (int k = 0; k < 8; ++k) {
+                for (int k = 0; k < 4 + half; ++k) {  // (the second half also has the sums)
                     uint32_t o[16];
-                    tmem_ld16(tq + cO + 16 * k, o);
+                    const uint32_t at = tq + (k < 4 ? cO + 64 * half + 16 * k : cL);
+                    tmem_ld16(at, o);
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                    tmem_st16(tq + cO + 16 * k, o);
+                    tmem_st16(at, o);
                 }
-                uint32_t o[16];
-                tmem_ld16(tq + cL, o);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                o[0] = __float_as_uint(__uint_as_float(o[0]) * f);
-                tmem_st16(tq + cL, o);
             };
             for (int j = 0; j < r.n; ++j, ++it) {
                 const uint32_t ts = tq + cS + (it & 1) * 128;
                 mb_wait(sm0 + oS + 8 * (it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, a.status);
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const int left = a.T - (r.t0 + j) * kSharedTile;
-                // 32 tokens at a time: the next ones are on their way out of tensor memory while these are worked on; P takes the place of
-                // scores that have been read
-                auto chunk = [&](int c, uint32_t (&s)[32], uint32_t (&next)[32]) {
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                    if (c < 3) tmem_ld32(ts + 32 * (c + 1), next);
-                    if (left < kSharedTile) {
+                uint32_t s[2][32];
+                tmem_ld32(ts + 64 * half, s[0]);
+                tmem_ld32(ts + 64 * half + 32, s[1]);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                const int left = a.T - (r.t0 + j) * kSharedTile - 64 * half;  // this half's tokens
+                if (left < 64) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (i >= left - 32 * c) s[i] = 0xFF800000u;
-                    }
-                    float mx[4] = {__uint_as_float(s[0]), __uint_as_float(s[1]), __uint_as_float(s[2]), __uint_as_float(s[3])};
-#pragma unroll
-                    for (int i = 4; i < 32; i += 8)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            mx[k] = i + 4 < 32 ? fmaxf(fmaxf(mx[k], __uint_as_float(s[i + k])), __uint_as_float(s[(i + 4 & 31) + k])) : fmaxf(mx[k], __uint_as_float(s[i + k]));
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ks;
-                    if (__any_sync(0xFFFFFFFFu, top > m + kLazy)) move_reference(top, j, c);
-                    uint32_t p[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float x, y;
-                        scaled2(s[2 * i], s[2 * i + 1], ks, -m, x, y);
-                        x = ex2(x);
-                        y = ex2(y);
-                        p[i] = pack2(x, y);
-                    }
-                    tmem_st16(ts + 16 * c, p);
-                };
-                uint32_t sa[32], sb[32];
-                tmem_ld32(ts, sa);
-#pragma unroll 1
-                for (int c = 0; c < 4; c += 2) {
-                    chunk(c, sa, sb);
-                    chunk(c + 1, sb, sa);
+                            if (32 * c + i >= left) s[c][i] = 0xFF800000u;
                 }
+                float mx[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    mx[k] = fmaxf(__uint_as_float(s[k & 1][16 * (k >> 1)]), __uint_as_float(s[k & 1][16 * (k >> 1) + 1]));
+#pragma unroll
+                    for (int i = 2; i < 16; i += 2)
+                        mx[k] = fmaxf(fmaxf(mx[k], __uint_as_float(s[k & 1][16 * (k >> 1) + i])), __uint_as_float(s[k & 1][16 * (k >> 1) + i + 1]));
+                }
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ks;
+                // (also says that the other half has read its scores: P of this one lies where they were)
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                if (pair_any(pair, top > m + kLazy)) move_reference(top, j);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                uint32_t p[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int k = 2 * i & 31;
+                    float x, y;
+                    scaled2(s[i >> 4][k], s[i >> 4][k + 1], ks, -m, x, y);
+                    p[i] = pack2(ex2(x), ex2(y));
+                }
+                tmem_st32(ts + 32 * half, p);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
@@ -477,23 +484,21 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             float* const part = a.partials + (int64_t)(blockIdx.x + r.u) * shared_part_floats(sch.row_tile, 128);
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 2 * half; c < 2 * half + 2; ++c) {
                 uint32_t o[32];
                 tmem_ld32(tq + cO + 32 * c, o);
                 asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                if ((int)threadIdx.x < rows)
+                if (row < rows)
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<float4*>(part + ((int64_t)(8 * c + i) * sch.row_tile + threadIdx.x) * 4) =
+                        *reinterpret_cast<float4*>(part + ((int64_t)(8 * c + i) * sch.row_tile + row) * 4) =
                             make_float4(__uint_as_float(o[4 * i]) * uscale, __uint_as_float(o[4 * i + 1]) * uscale, __uint_as_float(o[4 * i + 2]) * uscale,
                                         __uint_as_float(o[4 * i + 3]) * uscale);
             }
-            uint32_t sum[16];
-            tmem_ld16(tq + cL, sum);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-            if ((int)threadIdx.x < rows) {
-                part[(int64_t)sch.row_tile * 128 + threadIdx.x] = m * 0.6931471805599453f;  // the join works in natural-log units
-                part[(int64_t)sch.row_tile * 129 + threadIdx.x] = __uint_as_float(sum[0]);
+            const uint32_t sum = tmem_ld1(tq + cL);
+            if (half == 0 && row < rows) {
+                part[(int64_t)sch.row_tile * 128 + row] = m * 0.6931471805599453f;  // the join works in natural-log units
+                part[(int64_t)sch.row_tile * 129 + row] = __uint_as_float(sum);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         }
@@ -504,7 +509,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (warp == 13) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    if (warp == 17) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
 }  // namespace
