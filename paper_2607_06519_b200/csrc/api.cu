@@ -947,6 +947,7 @@ static fdkv_status shared_impl(fdkv_ctx* c, int32_t layer, int32_t prompt, const
     a.tail_len = arp<int32_t>(c, c->ar.tail_len) + (size_t)layer * s.max_batch;
     a.seqs = seqs; a.lens = c->host_tail.data();
     a.modes = c->seqs[prompt].modes.data() + (layer / s.B) * s.Hkv;
+    a.keep = (double)s.keep_num / s.keep_den;
     a.tmap = c->has_tmap ? c->tmap : nullptr;
     a.arena_base = c->arena;
     a.twice = c->packed_lists && s.B == 4;

@@ -400,11 +400,12 @@ cudaError_t launch_append_tail(const void* k, const void* v, int64_t stride_t, i
 constexpr int kMaxShared = 1024;     // sequences of one call
 constexpr int kSharedFew = 64;       // ... whose lists travel as a short parameter
 constexpr int kSharedTile = 128;     // prompt tokens per tile
-// The prompt part's work: items (KV head, group of query rows), item-major, of `tiles` tiles each, cut into one range per block.
-// Block c works on tiles [start[c], start[c + 1]) of that list; its part of item u has number c + u.
+// The prompt part's work: the flat list of (KV head, tile) is cut into ranges; the blocks of a range, one for each group of query rows, walk it
+// at the same time, so that its rows come out of L2 for all but the first.  Block c: range c / groups, group c % groups; its part
+// of head h has number (range + h) * groups + group.
 struct SharedSched {
-    int start[kMaxSplits + 1];
-    int ncta, tiles, groups, row_tile;  // blocks, tiles per item, row groups per KV head, query rows per group
+    int start[kMaxSplits + 1];  // head * tiles + tile; every range has a tile
+    int ranges, tiles, groups, row_tile;  // tiles per head, row groups, query rows per group
 };
 struct SharedArgs {
     const UnitDesc* desc;  // [Hkv] of the prompt and layer
@@ -417,6 +418,7 @@ struct SharedArgs {
     int32_t* tail_len;      // the layer's device copies of the lengths: [max_batch]
     const int32_t *seqs, *lens;  // HOST [batch]: slots, and their tail lengths with this call's append
     const int32_t* modes;   // HOST [Hkv]
+    double keep;            // residual keep fraction
     const void* tmap;       // CUtensorMap over the arena as rows of 256 bytes (bf16, head_dim 128), or null
     const void* arena_base;
     int twice;              // packed lists: the deviations of a block of four are stored doubled

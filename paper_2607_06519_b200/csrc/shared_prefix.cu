@@ -65,12 +65,12 @@ __global__ void __launch_bounds__(kThreads) shared_part_kernel(SharedArgs a, con
     asm volatile("griddepcontrol.wait;" ::: "memory");  // q belongs to the kernels ahead
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (behind the wait: the join reads the tails before its own)
     const int R = a.batch * a.G;
-    int g0 = sch.start[blockIdx.x];
-    const int g1 = sch.start[blockIdx.x + 1];
+    const int range = blockIdx.x / sch.groups, group = blockIdx.x % sch.groups, row0 = group * kRows, rows = min(kRows, R - row0);
+    int g0 = sch.start[range];
+    const int g1 = sch.start[range + 1];
     while (g0 < g1) {
-        const int u = g0 / sch.tiles, t_first = g0 % sch.tiles, t_last = min(sch.tiles, t_first + g1 - g0);
+        const int h = g0 / sch.tiles, t_first = g0 % sch.tiles, t_last = min(sch.tiles, t_first + g1 - g0);
         g0 += t_last - t_first;
-        const int h = u / sch.groups, row0 = (u % sch.groups) * kRows, rows = min(kRows, R - row0);
         const UnitDesc ud = a.desc[h];
         const bool resid = ud.mode == FDKV_MODE_RESIDUAL;
         const float kscale = ud.scale * rsqrtf((float)D), sign = ud.sign;
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kThreads) shared_part_kernel(SharedArgs a, con
             }
         }
         __syncthreads();
-        float* const part = a.partials + (int64_t)(blockIdx.x + u) * shared_part_floats(sch.row_tile, D);
+        float* const part = a.partials + ((int64_t)(range + h) * sch.groups + group) * shared_part_floats(sch.row_tile, D);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = ty + 16 * i;
@@ -215,14 +215,14 @@ struct SharedSeqs {
     int32_t slot[NB], len[NB];  // len counts this call's append
 };
 
-// Blocks [lo, hi] whose ranges meet item u.
-__device__ __forceinline__ void blocks_of_item(const SharedSched& sch, int u, int& lo, int& hi) {
+// Ranges [lo, hi] that meet head h.
+__device__ __forceinline__ void ranges_of_head(const SharedSched& sch, int h, int& lo, int& hi) {
     lo = 0;
     for (int step = 128; step; step >>= 1)
-        if (lo + step < sch.ncta && sch.start[lo + step] <= u * sch.tiles) lo += step;
+        if (lo + step < sch.ranges && sch.start[lo + step] <= h * sch.tiles) lo += step;
     hi = lo;
     for (int step = 128; step; step >>= 1)
-        if (hi + step < sch.ncta && sch.start[hi + step] < (u + 1) * sch.tiles) hi += step;
+        if (hi + step < sch.ranges && sch.start[hi + step] < (h + 1) * sch.tiles) hi += step;
 }
 
 // A softmax state: what the exponents are relative to (natural logarithm), their sum, four channels of the weighted sum.
@@ -235,7 +235,7 @@ struct State4 {
         a.x = a.x * f0 + o.x * f1; a.y = a.y * f0 + o.y * f1; a.z = a.z * f0 + o.z * f1; a.w = a.w * f0 + o.w * f1;
         m = mn;
     }
-    // parts c, c + step, .. up to hi of the row r of an item (p0: its part of block 0), BATCH of them on their way at a time
+    // parts c, c + step, .. up to hi of the row r of a group (p0: that of range 0; `stride` floats on: that of the next), BATCH of them on their way
     template <int D, int BATCH>
     __device__ __forceinline__ void add_parts(const float* p0, int64_t stride, int row_tile, int r, int c4, int c, int hi, int step) {
         for (; c <= hi; c += BATCH * step) {
@@ -385,15 +385,15 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(SharedArgs
             if (lane == 0) { s_m[warp][g] = M; s_l[warp][g] = l[g]; }
         }
     }
-    const int row0 = b * G, u = h * sch.groups + row0 / sch.row_tile, r0 = row0 % sch.row_tile;  // (row tiles hold whole sequences)
+    const int group = b * G / sch.row_tile, r0 = b * G - group * sch.row_tile;  // (row tiles hold whole sequences)
     int c_lo, c_hi;
-    blocks_of_item(sch, u, c_lo, c_hi);
+    ranges_of_head(sch, h, c_lo, c_hi);
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the prompt's parts
     const int i = threadIdx.x % ITEMS, way = threadIdx.x / ITEMS, g = i % G, c4 = i / G;
-    const int64_t stride = shared_part_floats(sch.row_tile, D);
+    const int64_t part = shared_part_floats(sch.row_tile, D), stride = sch.groups * part;
     State4 s;
-    s.add_parts<D, 6>(a.partials + u * stride, stride, sch.row_tile, r0 + g, c4, c_lo + way, c_hi, WAYS);
+    s.add_parts<D, 6>(a.partials + h * stride + group * part, stride, sch.row_tile, r0 + g, c4, c_lo + way, c_hi, WAYS);
     if constexpr (WAYS > 1) {
         j_acc[way][i] = s.a;
         j_ml[way][i] = make_float2(s.m, s.l);
@@ -473,9 +473,9 @@ __global__ void __launch_bounds__(kTcWarps * 32, 3) shared_join_tc_kernel(Shared
     const __nv_bfloat16* const kn = a.k_new ? reinterpret_cast<const __nv_bfloat16*>(a.k_new) + new0 : nullptr;
     const __nv_bfloat16* const vn = a.k_new ? reinterpret_cast<const __nv_bfloat16*>(a.v_new) + new0 : nullptr;
 
-    const int row0 = b * G, u = h * sch.groups + row0 / sch.row_tile, r0 = row0 % sch.row_tile;  // (row tiles hold whole sequences)
+    const int group = b * G / sch.row_tile, r0 = b * G - group * sch.row_tile;  // (row tiles hold whole sequences)
     int c_lo, c_hi;
-    blocks_of_item(sch, u, c_lo, c_hi);
+    ranges_of_head(sch, h, c_lo, c_hi);
 
     float o[8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -587,8 +587,8 @@ __global__ void __launch_bounds__(kTcWarps * 32, 3) shared_join_tc_kernel(Shared
     }
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the prompt's parts
-    const int64_t stride = shared_part_floats(sch.row_tile, D);
-    const float* const p0 = a.partials + u * stride;
+    const int64_t part = shared_part_floats(sch.row_tile, D), stride = sch.groups * part;
+    const float* const p0 = a.partials + h * stride + group * part;
 #pragma unroll
     for (int round = 0; round < ROUNDS; ++round) {
         const int i = (int)threadIdx.x % ITEMS + round * THREADS, way = threadIdx.x / ITEMS, g = i % G, c4 = i / G;
@@ -680,7 +680,7 @@ cudaError_t launch_join_tc(const SharedArgs& a, const SharedSched& sch, int sms,
     // blocks per unit: more than one while they leave half of the device idle and have parts or tail tokens for each
     int longest = 0;
     for (int b = 0; b < a.batch; ++b) longest = std::max(longest, a.lens[b]);
-    const int parts = std::max(1, sch.ncta / (a.Hkv * sch.groups));
+    const int parts = std::max(1, sch.ranges / a.Hkv);
     int ranks = 1;
     while (ranks < kMaxJoin && a.Hkv * a.batch * ranks <= sms && (parts >= 8 * ranks || longest >= 128 * ranks)) ranks *= 2;
     cudaLaunchAttribute attr[2];
@@ -705,21 +705,51 @@ cudaError_t launch_part(const SharedArgs& a, const SharedSched& sch, cudaStream_
     const cudaError_t e = once.ensure([]() { return cudaFuncSetAttribute(shared_part_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, part_smem<D>()); });
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute attr[1];
-    cudaLaunchConfig_t cfg = config(dim3(sch.ncta), kThreads, part_smem<D>(), st, attr);
+    cudaLaunchConfig_t cfg = config(dim3(sch.ranges * sch.groups), kThreads, part_smem<D>(), st, attr);
     return cudaLaunchKernelEx(&cfg, shared_part_kernel<T, D>, a, sch);
 }
 
-// Whole tiles to the blocks, as evenly as they go.
+// Whole tiles to the ranges, as evenly as their costs go.
 cudaError_t plan_shared(const SharedArgs& a, int row_tile, int sms, SharedSched& sch) {
     const int R = a.batch * a.G;
+    sms = std::min(sms, kMaxSplits);  // (what the partial sums have room for)
     sch.row_tile = std::min(row_tile, R);
     sch.groups = (R + row_tile - 1) / row_tile;
     sch.tiles = (a.T + kSharedTile - 1) / kSharedTile;
-    const int64_t total = (int64_t)a.Hkv * sch.groups * sch.tiles;
+    const int64_t total = (int64_t)a.Hkv * sch.tiles;
     if (total >= (int64_t)1 << 31) return cudaErrorInvalidValue;
-    sch.ncta = (int)std::min<int64_t>(std::min(sms, kMaxSplits), total);
-    for (int c = 0; c <= sch.ncta; ++c) sch.start[c] = (int)(total * c / sch.ncta);
-    const int64_t parts = sch.ncta + (int64_t)a.Hkv * sch.groups - 1;
+    // as many ranges as make one round of blocks, or, where one would leave SMs idle (more than 37 groups), two or three
+    int ranges = 1;
+    double best = 0.0;
+    for (int rounds = 1; rounds <= 3; ++rounds) {
+        const int n = std::min(rounds * sms / sch.groups, kMaxSplits);
+        const double used = n ? (double)n * sch.groups / (((n * sch.groups + sms - 1) / sms) * sms) : 0.0;
+        if (used > best + 0.1) {
+            best = used;
+            ranges = n;
+        }
+    }
+    sch.ranges = (int)std::min<int64_t>(ranges, total);
+    // A tile of a residual head takes longer by the products with its entries, and by their number: measured at 1/32, 1/16 and 1/8 kept, us a tile
+    // of 32 query rows 1.79, 1.88 and 2.29 against 1.63.
+    const double resid = 1.1 + 2.0 * a.keep;
+    double cost = 0.0;
+    for (int h = 0; h < a.Hkv; ++h) cost += sch.tiles * (a.modes[h] == FDKV_MODE_RESIDUAL ? resid : 1.0);
+    int h = 0;
+    double before = 0.0;  // cost of the heads before h
+    sch.start[0] = 0;
+    for (int c = 1; c < sch.ranges; ++c) {
+        const double at = cost * c / sch.ranges;
+        double w = a.modes[h] == FDKV_MODE_RESIDUAL ? resid : 1.0;
+        while (h + 1 < a.Hkv && at >= before + sch.tiles * w) {
+            before += sch.tiles * w;
+            w = a.modes[++h] == FDKV_MODE_RESIDUAL ? resid : 1.0;
+        }
+        const int64_t cut = (int64_t)h * sch.tiles + std::min<int64_t>(sch.tiles, (int64_t)((at - before) / w + 0.5));
+        sch.start[c] = (int)std::min<int64_t>(std::max<int64_t>(cut, sch.start[c - 1] + 1), total - (sch.ranges - c));
+    }
+    sch.start[sch.ranges] = (int)total;
+    const int64_t parts = ((int64_t)sch.ranges + a.Hkv - 1) * sch.groups;
     return parts * shared_part_floats(sch.row_tile, a.d) <= a.partial_floats ? cudaSuccess : cudaErrorInvalidValue;
 }
 

@@ -1,7 +1,7 @@
 // The prompt part of decode attention on one shared prompt, bf16 / head_dim 128 (see shared_prefix.cu): the query rows of all
 // sequences of a KV head fill the rows of tcgen05 products, so that a tile of the compressed prompt is read once and used by up to 128 rows.
 //
-// A persistent block per SM walks a range of the flat (KV head, row group, 128-token tile) list:
+// A persistent block per SM walks a range of the flat (KV head, 128-token tile) list for one group of 128 query rows:
 //   warp 16    TMA producer: the tile's K and V rows (2 x 64 channels x 128 tokens, 128-byte swizzle)
 //   warps 8-15 residual units: the tile's kept entries of K (8-11) and V (12-15), scattered into a zeroed tile of the same layout (32
 //              tokens per warp)
@@ -114,17 +114,15 @@ __device__ __forceinline__ void st_v4(uint32_t addr, uint32_t a, uint32_t b, uin
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// What of a block's range every role walks: runs of tiles of one item.
+// What of a block's range every role walks: runs of tiles of one head.
 struct Run {
-    int u, h, row0, t0, n;
+    int h, t0, n;
 };
 __device__ __forceinline__ bool next_run(const SharedSched& sch, int& g, int g_end, Run& r) {
     if (g >= g_end) return false;
-    r.u = g / sch.tiles;
-    r.t0 = g - r.u * sch.tiles;
+    r.h = g / sch.tiles;
+    r.t0 = g - r.h * sch.tiles;
     r.n = min(sch.tiles - r.t0, g_end - g);
-    r.h = r.u / sch.groups;
-    r.row0 = (r.u - r.h * sch.groups) * 128;
     g += r.n;
     return true;
 }
@@ -169,8 +167,9 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + oTmem);
-    int g = sch.start[blockIdx.x];
-    const int g_end = sch.start[blockIdx.x + 1];
+    const int range = blockIdx.x / sch.groups, group = blockIdx.x - range * sch.groups, row0 = group * 128;
+    int g = sch.start[range];
+    const int g_end = sch.start[range + 1];
     Run r;
     // Slots in ring order: K (and its entries) of tile 0, then for every tile j: K of tile j + 1, V of tile j.
     int sl = 0;
@@ -384,11 +383,11 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (behind the wait: the join reads the tails before its own)
         int it = 0;
         while (next_run(sch, g, g_end, r)) {
-            const int rows = min(128, a.batch * a.G - r.row0);
+            const int rows = min(128, a.batch * a.G - row0);
             const float uscale = a.desc[r.h].scale;
             const float ks = uscale * (0.08838834764831845f * 1.4426950408889634f);  // / sqrt(128), in powers of two
             {
-                const int i = r.row0 + row, b = i / a.G;
+                const int i = row0 + row, b = i / a.G;
                 const char* const src = reinterpret_cast<const char*>(a.q) + (((int64_t)b * a.Hq + r.h * a.G + (i - b * a.G)) << 8) + 128 * half;
                 uint32_t x[32];
 #pragma unroll
@@ -482,7 +481,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             mb_wait(sm0 + oO + 8 * ((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, abort_flag, a.status);
             __syncwarp();
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            float* const part = a.partials + (int64_t)(blockIdx.x + r.u) * shared_part_floats(sch.row_tile, 128);
+            float* const part = a.partials + ((int64_t)(range + r.h) * sch.groups + group) * shared_part_floats(sch.row_tile, 128);
 #pragma unroll 1
             for (int c = 2 * half; c < 2 * half + 2; ++c) {
                 uint32_t o[32];
@@ -519,7 +518,7 @@ cudaError_t launch_shared_tc(const SharedArgs& a, const SharedSched& sch, cudaSt
     const cudaError_t e = once.ensure([]() { return cudaFuncSetAttribute(shared_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(sch.ncta);
+    cfg.gridDim = dim3(sch.ranges * sch.groups);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = st;
