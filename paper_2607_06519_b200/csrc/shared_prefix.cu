@@ -441,9 +441,9 @@ __device__ __forceinline__ float4 peer_load4(uint32_t addr) {
     asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ float2 peer_load2(uint32_t addr) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+__device__ __forceinline__ float peer_load(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
 
@@ -456,13 +456,12 @@ __device__ __forceinline__ float2 peer_load2(uint32_t addr) {
 template <int G, int NB>
 __global__ void __launch_bounds__(kTcWarps * 32, 3) shared_join_tc_kernel(SharedArgs a, const __grid_constant__ SharedSched sch, const __grid_constant__ SharedSeqs<NB> sq) {
     constexpr int D = 128, ITEMS = G * D / 4, THREADS = kTcWarps * 32;
-    constexpr int WAYS = THREADS / ITEMS > 0 ? THREADS / ITEMS : 1, ROUNDS = ITEMS > THREADS ? ITEMS / THREADS : 1;
     constexpr bool SPLIT = G <= 4;
     __shared__ __align__(16) float s_acc[kTcWarps][G][D];
     __shared__ float s_m[kTcWarps][G], s_l[kTcWarps][G];
-    __shared__ __align__(16) float4 j_acc[WAYS][ITEMS];  // (in clusters the block's state, in row 0)
-    __shared__ __align__(16) float2 j_ml[WAYS][ITEMS];
-    const int rank = blockIdx.x, ranks = gridDim.x, h = blockIdx.y, b = blockIdx.z;
+    __shared__ float4 j_acc[THREADS];
+    __shared__ float2 j_ml[THREADS];
+    const int rank = blockIdx.x, ranks = (int)gridDim.x, h = blockIdx.y, b = blockIdx.z;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int n = sq.len[b], slot = sq.slot[b];
@@ -585,55 +584,46 @@ __global__ void __launch_bounds__(kTcWarps * 32, 3) shared_join_tc_kernel(Shared
             }
         }
     }
-    __syncthreads();
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the prompt's parts
+    // ---- fours of outputs: this block's share of the unit's, each over as many threads as there are; first the tail's states, those of the
+    // cluster's other blocks among them, then, when it is there, the prompt ----
+    const int share = ITEMS / ranks, ways = share < THREADS ? THREADS / share : 1;
+    if (ranks > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    else __syncthreads();
     const int64_t part = shared_part_floats(sch.row_tile, D), stride = sch.groups * part;
     const float* const p0 = a.partials + h * stride + group * part;
+    constexpr int ROUNDS = ITEMS > THREADS ? ITEMS / THREADS : 1;  // (more than one: ranks == 1 or a share that still is one)
+    State4 s[ROUNDS];
+    const int way = threadIdx.x / share;
 #pragma unroll
     for (int round = 0; round < ROUNDS; ++round) {
-        const int i = (int)threadIdx.x % ITEMS + round * THREADS, way = threadIdx.x / ITEMS, g = i % G, c4 = i / G;
-        State4 s;
-        s.add_parts<D, 6>(p0, stride, sch.row_tile, r0 + g, c4, c_lo + rank + way * ranks, c_hi, WAYS * ranks);
-        if constexpr (WAYS > 1) {
-            j_acc[way][i] = s.a;
-            j_ml[way][i] = make_float2(s.m, s.l);
+        const int k = (int)threadIdx.x % share + round * THREADS, i = rank * share + k, g = i % G, c4 = i / G;
+        if (k < share)
+            for (int e = way; e < kTcWarps * ranks; e += ways) {
+                const int w = e % kTcWarps, c = e / kTcWarps;
+                if (ranks == 1) {
+                    s[round].add(s_m[w][g], s_l[w][g], *reinterpret_cast<const float4*>(&s_acc[w][g][c4 * 4]));
+                } else {
+                    s[round].add(peer_load(peer_addr(&s_m[w][g], c)), peer_load(peer_addr(&s_l[w][g], c)), peer_load4(peer_addr(&s_acc[w][g][c4 * 4], c)));
+                }
+            }
+    }
+    if (ranks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (the peers' states have been read; awaited at the end)
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the prompt's parts
+#pragma unroll
+    for (int round = 0; round < ROUNDS; ++round) {
+        if (round > 0 && share <= THREADS) break;
+        const int k = (int)threadIdx.x % share + round * THREADS, i = rank * share + k, g = i % G, c4 = i / G;
+        if (k < share) s[round].add_parts<D, 6>(p0, stride, sch.row_tile, r0 + g, c4, c_lo + way, c_hi, ways);
+        if (ways > 1) {  // (one round)
+            j_acc[threadIdx.x] = s[round].a;
+            j_ml[threadIdx.x] = make_float2(s[round].m, s[round].l);
             __syncthreads();
             if (way == 0)
-#pragma unroll
-                for (int w = 1; w < WAYS; ++w) s.add(j_ml[w][i].x, j_ml[w][i].y, j_acc[w][i]);
+                for (int w = 1; w < ways; ++w) s[round].add(j_ml[w * share + k].x, j_ml[w * share + k].y, j_acc[w * share + k]);
         }
-        if (way == 0) {
-#pragma unroll
-            for (int w = 0; w < kTcWarps; ++w) s.add(s_m[w][g], s_l[w][g], *reinterpret_cast<const float4*>(&s_acc[w][g][c4 * 4]));
-            if (ranks == 1) {
-                s.store(a.out, a.out_dtype, ((int64_t)b * a.Hq + h * G + g) * D + c4 * 4);
-            } else {
-                j_acc[0][i] = s.a;
-                j_ml[0][i] = make_float2(s.m, s.l);
-            }
-        }
+        if (way == 0 && k < share) s[round].store(a.out, a.out_dtype, ((int64_t)b * a.Hq + h * G + g) * D + c4 * 4);
     }
-    if (ranks == 1) return;
-    // ---- the cluster's blocks: each joins and writes its share of the outputs ----
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    const int share = ITEMS / ranks;
-    for (int k = threadIdx.x; k < share; k += THREADS) {
-        const int i = rank * share + k;
-        float4 pa[kMaxJoin];
-        float2 pm[kMaxJoin];
-#pragma unroll
-        for (int c = 0; c < kMaxJoin; ++c)
-            if (c < ranks) {
-                pa[c] = peer_load4(peer_addr(&j_acc[0][i], c));
-                pm[c] = peer_load2(peer_addr(&j_ml[0][i], c));
-            }
-        State4 s;
-#pragma unroll
-        for (int c = 0; c < kMaxJoin; ++c)
-            if (c < ranks) s.add(pm[c].x, pm[c].y, pa[c]);
-        s.store(a.out, a.out_dtype, ((int64_t)b * a.Hq + h * G + i % G) * D + i / G * 4);
-    }
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");  // (the peers have read this block's state)
+    if (ranks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t st, cudaLaunchAttribute* attr) {
