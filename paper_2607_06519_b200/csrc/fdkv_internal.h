@@ -399,7 +399,7 @@ cudaError_t launch_append_tail(const void* k, const void* v, int64_t stride_t, i
 // ---- decode attention of a batch on one committed prompt (shared_prefix.cu, shared_tc.cu) ----
 constexpr int kMaxShared = 1024;     // sequences of one call
 constexpr int kSharedFew = 64;       // ... whose lists travel as a short parameter
-constexpr int kSharedTile = 128;     // prompt tokens per tile
+constexpr int kSharedTile = 128;     // prompt tokens per tile (tensor-core kernel)
 // The prompt part's work: the flat list of (KV head, tile) is cut into ranges; the blocks of a range, one for each group of query rows, walk it
 // at the same time, so that its rows come out of L2 for all but the first.  Block c: range c / groups, group c % groups; its part
 // of head h has number (range + h) * groups + group.

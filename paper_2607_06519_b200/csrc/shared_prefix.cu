@@ -39,7 +39,7 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&f)[8]) {
 
 // ------------------------------------------------------------------------------------------------ prompt part, portable
 constexpr int kRows = 32;      // query rows of a group
-constexpr int kTok = 32;       // tokens at a time
+constexpr int kTok = 32;       // tokens at a time: a tile of the schedule
 constexpr int kThreads = 256;
 
 template <int D>
@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(kThreads) shared_part_kernel(SharedArgs a, con
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) o[i][j] = 0.f;
-        const int tok_end = min(ud.T, t_last * kSharedTile);
-        for (int tok = t_first * kSharedTile; tok < tok_end; tok += kTok) {
+        const int tok_end = min(ud.T, t_last * kTok);
+        for (int tok = t_first * kTok; tok < tok_end; tok += kTok) {
             const int n = min(kTok, tok_end - tok);
             __syncthreads();
             for (int i = tid; i < 2 * kTok * D / 8; i += kThreads) {
@@ -700,12 +700,12 @@ cudaError_t launch_part(const SharedArgs& a, const SharedSched& sch, cudaStream_
 }
 
 // Whole tiles to the ranges, as evenly as their costs go.
-cudaError_t plan_shared(const SharedArgs& a, int row_tile, int sms, SharedSched& sch) {
+cudaError_t plan_shared(const SharedArgs& a, int row_tile, int tile, int sms, SharedSched& sch) {
     const int R = a.batch * a.G;
     sms = std::min(sms, kMaxSplits);  // (what the partial sums have room for)
     sch.row_tile = std::min(row_tile, R);
     sch.groups = (R + row_tile - 1) / row_tile;
-    sch.tiles = (a.T + kSharedTile - 1) / kSharedTile;
+    sch.tiles = (a.T + tile - 1) / tile;
     const int64_t total = (int64_t)a.Hkv * sch.tiles;
     if (total >= (int64_t)1 << 31) return cudaErrorInvalidValue;
     // as many ranges as make one round of blocks, or, where one would leave SMs idle (more than 37 groups), two or three
@@ -752,7 +752,7 @@ cudaError_t launch_shared_decode(const SharedArgs& a, int dtype, cudaStream_t st
     if (e != cudaSuccess) return e;
     SharedSched sch;
     const bool tc = a.tmap != nullptr;
-    if ((e = plan_shared(a, tc ? 128 : kRows, sms, sch)) != cudaSuccess) return e;
+    if ((e = (tc ? plan_shared(a, 128, kSharedTile, sms, sch) : plan_shared(a, kRows, kTok, sms, sch))) != cudaSuccess) return e;
     if (tc) {
         e = launch_shared_tc(a, sch, st);
         if (e == cudaSuccess) e = a.batch <= kSharedFew ? launch_join_tc<kSharedFew>(a, sch, sms, st) : launch_join_tc<kMaxShared>(a, sch, sms, st);
