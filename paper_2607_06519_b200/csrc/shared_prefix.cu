@@ -699,6 +699,8 @@ cudaError_t launch_part(const SharedArgs& a, const SharedSched& sch, cudaStream_
     return cudaLaunchKernelEx(&cfg, shared_part_kernel<T, D>, a, sch);
 }
 
+// us per tile of 128 tokens: with entries (and per kept fraction), without them when memory bounds all blocks, one or more row groups, and when it does not
+constexpr double kSlowTile = 1.75, kSlowKept = 4.4, kMeanTile = 1.62, kGroupTile = 1.15, kFastTile = 1.0;
 // Whole tiles to the ranges, as evenly as their costs go.
 cudaError_t plan_shared(const SharedArgs& a, int row_tile, int tile, int sms, SharedSched& sch) {
     const int R = a.batch * a.G;
@@ -720,9 +722,12 @@ cudaError_t plan_shared(const SharedArgs& a, int row_tile, int tile, int sms, Sh
         }
     }
     sch.ranges = (int)std::min<int64_t>(ranges, total);
-    // A tile of a residual head takes longer by the products with its entries, and by their number: measured at 1/32, 1/16 and 1/8 kept, us a tile
-    // of 32 query rows 1.79, 1.88 and 2.29 against 1.63.
-    const double resid = 1.1 + 2.0 * a.keep;
+    // A block takes `slow` us for a tile with entries, whatever the others do, and for one without as long as the memory needs on average, or
+    // less where blocks that are slower leave it room: that share of the time is what the others then take.
+    int n_slow = 0;
+    for (int h = 0; h < a.Hkv; ++h) n_slow += a.modes[h] == FDKV_MODE_RESIDUAL;
+    const double f = (double)n_slow / a.Hkv, slow = kSlowTile + kSlowKept * a.keep, mean = sch.groups > 1 ? kGroupTile : kMeanTile;
+    const double plain = n_slow < a.Hkv ? std::max(kFastTile, (mean - f * slow) / (1.0 - f)) : mean, resid = slow / plain;
     double cost = 0.0;
     for (int h = 0; h < a.Hkv; ++h) cost += sch.tiles * (a.modes[h] == FDKV_MODE_RESIDUAL ? resid : 1.0);
     int h = 0;
