@@ -244,10 +244,15 @@ struct State4 {
 #pragma unroll
             for (int k = 0; k < BATCH; ++k) {
                 const int cc = c + k * step;
-                const float* const part = p0 + (cc <= hi ? cc : c) * stride;
-                pm[k] = cc <= hi ? __ldcg(part + (int64_t)row_tile * D + r) : -INFINITY;
-                pl[k] = __ldcg(part + (int64_t)row_tile * (D + 1) + r);
-                po[k] = __ldcg(reinterpret_cast<const float4*>(part + ((int64_t)c4 * row_tile + r) * 4));
+                pm[k] = -INFINITY;
+                pl[k] = 0.f;
+                po[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (cc <= hi) {
+                    const float* const part = p0 + cc * stride;
+                    pm[k] = __ldcg(part + (int64_t)row_tile * D + r);
+                    pl[k] = __ldcg(part + (int64_t)row_tile * (D + 1) + r);
+                    po[k] = __ldcg(reinterpret_cast<const float4*>(part + ((int64_t)c4 * row_tile + r) * 4));
+                }
             }
             float mn = m;
 #pragma unroll
@@ -613,7 +618,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 3) shared_join_tc_kernel(Shared
     for (int round = 0; round < ROUNDS; ++round) {
         if (round > 0 && share <= THREADS) break;
         const int k = (int)threadIdx.x % share + round * THREADS, i = rank * share + k, g = i % G, c4 = i / G;
-        if (k < share) s[round].add_parts<D, 6>(p0, stride, sch.row_tile, r0 + g, c4, c_lo + way, c_hi, ways);
+        if (k < share) s[round].add_parts<D, 10>(p0, stride, sch.row_tile, r0 + g, c4, c_lo + way, c_hi, ways);
         if (ways > 1) {  // (one round)
             j_acc[threadIdx.x] = s[round].a;
             j_ml[threadIdx.x] = make_float2(s[round].m, s[round].l);
