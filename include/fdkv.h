@@ -237,15 +237,18 @@ fdkv_status fdkv_decode_step_host(fdkv_ctx* ctx, int32_t batch, const void* q /*
  * seqs: HOST int32[batch], distinct slots, batch <= 1024; each is prompt_seq itself (which then goes on with its own tail) or a
  * slot without a committed prompt (FDKV_ERR_STATE).  A sequence may have no tail rows at all.  The prompt is what the slot holds
  * committed at the time of the call: after fdkv_fold_tail on it, the folded tokens belong to it for every sequence.
- * bf16 storage with head_dim 128: the probabilities are rounded to bf16 for the second product (float32 sums), so that out is
- * within about 2e-3 of the exact attention; float32 storage: 1e-6.  FDKV_ROWS_E4M3 contexts: FDKV_ERR_UNSUPPORTED.
+ * bf16 storage with head_dim 128: the prompt's probabilities are rounded to bf16 for the second product (float32 sums), so that out is
+ * within about 1e-3 of the exact attention before its own rounding; the rest in float32 (1e-6).  FDKV_ROWS_E4M3 contexts: FDKV_ERR_UNSUPPORTED.
+ * Like fdkv_decode_attn's, a call's split-K parts lie in the workspace: calls of one context on several streams, replays of
+ * captured ones among them, are ordered by the caller.
  */
 fdkv_status fdkv_decode_attn_shared(fdkv_ctx* ctx, int32_t layer, int32_t prompt_seq, const int32_t* seqs /*HOST*/, int32_t batch, const void* q,
                                     const void* k_new, const void* v_new, void* out, int32_t out_dtype, void* stream);
 
 /* Appends n rows to one layer's tail of a sequence slot, committed or not (a sequence's own tokens behind a shared prompt): element
  * (t, h, ch) of k / v at ptr + t * stride_t + h * stride_h + ch, t < n, as in fdkv_compress_prefill.  FDKV_ERR_STATE where the tail
- * has no room for them.  n = 0 does nothing.  May not be captured into a graph that is replayed (the length is the host's).     */
+ * has no room for them.  n = 0 does nothing.  A prompt committed into the slot afterwards goes before these rows.  Issued on the stream, not captured
+ * (the length is the host's).                                                                                                    */
 fdkv_status fdkv_append_tail(fdkv_ctx* ctx, int32_t layer, int32_t seq, int32_t n, const void* k, const void* v, int64_t stride_t, int64_t stride_h,
                              void* stream);
 
@@ -287,7 +290,8 @@ fdkv_status fdkv_qk_norm_rope(const fdkv_rotary* r /*HOST*/, int64_t n, const vo
  * NULL: slots 0 .. batch-1, each on its own prompt) or fdkv_decode_attn_shared (prompt_seq >= 0), which appends the new rows.
  * qkv: [batch] rows, `stride` elements apart (a multiple of 8, >= (n_q_heads + 2 n_kv_heads) * head_dim), each the query heads, the key heads and the value
  * heads one after the other.  positions: DEVICE int32 [n_axes][batch], dense.  r's heads, head_dim and dtype are the context's.
- * Between the steps the rows lie in the context's workspace (the staging of the *_host calls).
+ * Between the steps the rows lie in the context's workspace (the staging of the *_host calls).  The call appends, so that it is issued
+ * on the stream, not captured (see fdkv_decode_attn).
  */
 fdkv_status fdkv_decode_qkv(fdkv_ctx* ctx, int32_t layer, int32_t prompt_seq, const int32_t* seqs /*HOST*/, int32_t batch, const fdkv_rotary* r /*HOST*/,
                             const void* qkv, int64_t stride, const int32_t* positions, void* out, int32_t out_dtype, void* stream);

@@ -39,6 +39,15 @@ fdkv_status fdkv_test_plan_clusters(int32_t batch, int32_t n_kv_heads, int32_t g
                                     const int32_t* max_clusters, uint32_t* start_out, int32_t* n_ctas_out, int32_t* cluster_out);
 
 /*
+ * Host-only: the cut of fdkv_decode_attn_shared on a device of `sms` SMs for a prompt of T tokens, `batch` sequences with `group` query heads per KV
+ * head, row_tile query rows per row group and `tile` tokens per tile; modes (HOST, [n_kv_heads]).  start_out (HOST, at least 161):
+ * the ranges of the (head, tile) list; counts_out (HOST, [4]): ranges, tiles per head, row groups, rows per group.  FDKV_ERR_WORKSPACE where
+ * max_batch sequences' partial sums would not hold it.
+ */
+fdkv_status fdkv_test_plan_shared(int32_t T, int32_t batch, int32_t max_batch, int32_t group, int32_t n_kv_heads, int32_t head_dim, const int32_t* modes, int32_t keep_num,
+                                  int32_t keep_den, int32_t row_tile, int32_t tile, int32_t sms, int32_t* start_out, int32_t* counts_out);
+
+/*
  * The per-device set-up table of the launchers (function attributes are per device, not per process), driven with a
  * list of device ids instead of the current device: returns how many of the n visits `devs` (HOST) would run the
  * set-up on a fresh table.  Host only; no GPU is touched.

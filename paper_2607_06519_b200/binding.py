@@ -75,6 +75,7 @@ def _load():
         "fdkv_device_status": [vp],
         "fdkv_compress_unit_noalloc": [vp, vp, i64, i32, i32, i32, i32, i32, vp, vp, vp, P(i32), vp],
         "fdkv_test_wait_expiry": [vp, i32, vp],
+        "fdkv_test_plan_shared": [i32] * 6 + [vp] + [i32] * 5 + [vp, vp],
         "fdkv_test_clear_device_status": [vp, vp],
     }
     for name, args in sig.items():
@@ -246,6 +247,8 @@ def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream
     """Norm and rotation of queries [n, n_q_heads, d] and keys [n, n_kv_heads, d] (either may be None); returns (q_out, k_out).
     Tensors may be strided (a slice of the fused projection, a layer's rows); an output may be its own input."""
     x = q if q is not None else k
+    if x is None:
+        raise ValueError("queries or keys are needed")
     n, _, d = x.shape
     dtype = x.dtype
     q_args = q_to = k_args = k_to = _NO_ROWS
@@ -263,6 +266,10 @@ def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream
         if k_out.shape[1] != hk:
             raise ValueError("k_out must have the shape of k")
     step = _positions(positions, rotary.n_axes, n) if positions is not None else 0
+    _on_device(x.get_device(), q, k, q_out, k_out, positions, rotary.q_weight, rotary.k_weight)
+    if x.get_device() != torch._C._cuda_getDevice():
+        with torch.cuda.device(x.device):
+            return qk_norm_rope(rotary, q, k, positions, q_out, k_out, stream)
     st = _qk_norm_rope(rotary.c(hq, hk, d, dtype), n, *q_args, *k_args, None if positions is None else positions.data_ptr(), step, *q_to, *k_to, _stream(stream))
     if st:
         raise FdkvError(st, "fdkv_qk_norm_rope")
@@ -270,6 +277,12 @@ def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream
 
 
 _NO_ROWS = (None, 0, 0)
+
+
+def _on_device(device: int, *tensors):
+    for t in tensors:
+        if t is not None and (t.get_device() != device or device < 0):
+            raise ValueError("all tensors must be on one CUDA device")
 
 
 def _rows(t, n: int, d: int, dtype):
@@ -392,6 +405,7 @@ class Context:
         slots, n, _keep = _slots(seqs)
         if len(q) != n:
             raise ValueError("q needs one row per sequence")
+        _on_device(self.arena.get_device(), q, k_new, v_new, out)
         if out is None:
             out = torch.empty(q.shape, dtype=torch.bfloat16 if od == BF16 else torch.float32, device=self.device)
         st = _decode_attn_shared(self.h, layer, prompt_seq, slots, n, q.data_ptr(), None if k_new is None else k_new.data_ptr(),
@@ -413,6 +427,7 @@ class Context:
         slots, ns, _keep = (None, n, None) if seqs is None else _slots(seqs)
         if ns != n:
             raise ValueError("qkv needs one row per sequence")
+        _on_device(self.arena.get_device(), qkv, positions, rotary.q_weight, rotary.k_weight, out)
         if out is None:
             out = torch.empty((n, c.n_q_heads, c.head_dim), dtype=torch.bfloat16 if od == BF16 else torch.float32, device=self.device)
         _check(_lib.fdkv_decode_qkv(self.h, layer, prompt_seq, slots, n, rotary.c(c.n_q_heads, c.n_kv_heads, c.head_dim, self.tdtype), qkv.data_ptr(),
@@ -424,6 +439,7 @@ class Context:
         if k.shape != v.shape or k.stride() != v.stride() or k.dtype is not self.tdtype or v.dtype is not self.tdtype or k.stride(2) != 1 or \
                 tuple(k.shape[1:]) != (self.cfg.n_kv_heads, self.cfg.head_dim):
             raise ValueError("k and v must share one [n, Hkv, d] strided layout and the context dtype")
+        _on_device(self.arena.get_device(), k, v)
         n, d = len(k), self.cfg.head_dim
         _check(_lib.fdkv_append_tail(self.h, layer, seq, n, _ptr(k), _ptr(v), k.stride(0) if n > 1 else d, k.stride(1) if k.shape[1] > 1 else d, _stream(stream)),
                "fdkv_append_tail")

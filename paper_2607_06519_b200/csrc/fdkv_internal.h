@@ -400,6 +400,7 @@ cudaError_t launch_append_tail(const void* k, const void* v, int64_t stride_t, i
 constexpr int kMaxShared = 1024;     // sequences of one call
 constexpr int kSharedFew = 64;       // ... whose lists travel as a short parameter
 constexpr int kSharedTile = 128;     // prompt tokens per tile (tensor-core kernel)
+constexpr int kSharedRows = 128;     // query rows per group (tensor-core kernel)
 // The prompt part's work: the flat list of (KV head, tile) is cut into ranges; the blocks of a range, one for each group of query rows, walk it
 // at the same time, so that its rows come out of L2 for all but the first.  Block c: range c / groups, group c % groups; its part
 // of head h has number (range + h) * groups + group.
@@ -428,6 +429,8 @@ struct SharedArgs {
 };
 inline __host__ __device__ int64_t shared_part_floats(int row_tile, int d) { return (int64_t)row_tile * (d + 4); }
 cudaError_t launch_shared_decode(const SharedArgs& a, int dtype, cudaStream_t st);
+// The cut of a call on a device of `sms` SMs; host only.
+cudaError_t plan_shared_decode(const SharedArgs& a, int row_tile, int tile, int sms, SharedSched& sch);
 
 // Function attributes (the opt-in to large dynamic shared memory) and the SM count belong to a device, not to the
 // process: every launcher keeps one of these and runs its set-up the first time it meets the current device.

@@ -704,10 +704,12 @@ cudaError_t launch_part(const SharedArgs& a, const SharedSched& sch, cudaStream_
     return cudaLaunchKernelEx(&cfg, shared_part_kernel<T, D>, a, sch);
 }
 
+}  // namespace
+
 // us per tile of 128 tokens: with entries (and per kept fraction), without them when memory bounds all blocks, one or more row groups, and when it does not
-constexpr double kSlowTile = 1.75, kSlowKept = 4.4, kMeanTile = 1.62, kGroupTile = 1.15, kFastTile = 1.0;
+static constexpr double kSlowTile = 1.75, kSlowKept = 4.4, kMeanTile = 1.62, kGroupTile = 1.15, kFastTile = 1.0;
 // Whole tiles to the ranges, as evenly as their costs go.
-cudaError_t plan_shared(const SharedArgs& a, int row_tile, int tile, int sms, SharedSched& sch) {
+cudaError_t plan_shared_decode(const SharedArgs& a, int row_tile, int tile, int sms, SharedSched& sch) {
     const int R = a.batch * a.G;
     sms = std::min(sms, kMaxSplits);  // (what the partial sums have room for)
     sch.row_tile = std::min(row_tile, R);
@@ -753,8 +755,6 @@ cudaError_t plan_shared(const SharedArgs& a, int row_tile, int tile, int sms, Sh
     return parts * shared_part_floats(sch.row_tile, a.d) <= a.partial_floats ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-}  // namespace
-
 cudaError_t launch_shared_decode(const SharedArgs& a, int dtype, cudaStream_t st) {
     static PerDevice once;
     int sms = 0;
@@ -762,7 +762,7 @@ cudaError_t launch_shared_decode(const SharedArgs& a, int dtype, cudaStream_t st
     if (e != cudaSuccess) return e;
     SharedSched sch;
     const bool tc = a.tmap != nullptr;
-    if ((e = (tc ? plan_shared(a, 128, kSharedTile, sms, sch) : plan_shared(a, kRows, kTok, sms, sch))) != cudaSuccess) return e;
+    if ((e = (tc ? plan_shared_decode(a, kSharedRows, kSharedTile, sms, sch) : plan_shared_decode(a, kRows, kTok, sms, sch))) != cudaSuccess) return e;
     if (tc) {
         e = launch_shared_tc(a, sch, st);
         if (e == cudaSuccess) e = a.batch <= kSharedFew ? launch_join_tc<kSharedFew>(a, sch, sms, st) : launch_join_tc<kMaxShared>(a, sch, sms, st);

@@ -307,7 +307,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 for (int i = 0; i < kPF; ++i)
                     if (e0 + lane + 32 * i < e1) pe[i] = (uint32_t)idx[e0 + lane + 32 * i];
                 // (about where the list is two tiles on: the slices' counts are much alike)
-                const int ahead = e0 + (e1 - e0) * 8 + lane * 32;
+                const int64_t ahead = (int64_t)e0 + (e1 - e0) * 8 + lane * 32;
                 if (lane * 32 < (e1 - e0) + 64 && ahead < list_end) asm volatile("prefetch.global.L2 [%0];" ::"l"(idx + ahead));
             };
             auto fill = [&](int j) {

@@ -71,6 +71,24 @@ fdkv_status fdkv_test_plan_clusters(int32_t batch, int32_t n_kv_heads, int32_t g
     return e == cudaSuccess ? FDKV_OK : FDKV_ERR_INVALID_ARG;
 }
 
+fdkv_status fdkv_test_plan_shared(int32_t T, int32_t batch, int32_t max_batch, int32_t group, int32_t n_kv_heads, int32_t head_dim, const int32_t* modes, int32_t keep_num,
+                                  int32_t keep_den, int32_t row_tile, int32_t tile, int32_t sms, int32_t* start_out, int32_t* counts_out) {
+    if (!modes || !start_out || !counts_out || T < 1 || batch < 1 || max_batch < batch || group < 1 || n_kv_heads < 1 || head_dim < 1 || keep_den < 1 || row_tile < 1 ||
+        tile < 1 || sms < 1)
+        return FDKV_ERR_INVALID_ARG;
+    fdkv::SharedArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.T = T; a.batch = batch; a.G = group; a.Hkv = n_kv_heads; a.Hq = n_kv_heads * group; a.d = head_dim;
+    a.modes = modes;
+    a.keep = (double)keep_num / keep_den;
+    a.partial_floats = (int64_t)max_batch * a.Hq * fdkv::kMaxSplits * (head_dim + 4);
+    fdkv::SharedSched sch;
+    if (fdkv::plan_shared_decode(a, row_tile, tile, sms, sch) != cudaSuccess) return FDKV_ERR_WORKSPACE;
+    for (int c = 0; c <= sch.ranges; ++c) start_out[c] = sch.start[c];
+    counts_out[0] = sch.ranges; counts_out[1] = sch.tiles; counts_out[2] = sch.groups; counts_out[3] = sch.row_tile;
+    return FDKV_OK;
+}
+
 int32_t fdkv_test_per_device_visits(const int32_t* devs, int32_t n) {
     if (!devs || n < 0) return -1;
     return fdkv::per_device_first_visits(reinterpret_cast<const int*>(devs), n);
