@@ -266,9 +266,10 @@ def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream
         if k_out.shape[1] != hk:
             raise ValueError("k_out must have the shape of k")
     step = _positions(positions, rotary.n_axes, n) if positions is not None else 0
-    _on_device(x.get_device(), q, k, q_out, k_out, positions, rotary.q_weight, rotary.k_weight)
-    if x.get_device() != torch._C._cuda_getDevice():
-        with torch.cuda.device(x.device):
+    device = x.get_device()
+    _on_device(device, q, k, q_out, k_out, positions, rotary.q_weight, rotary.k_weight)
+    if device != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
             return qk_norm_rope(rotary, q, k, positions, q_out, k_out, stream)
     st = _qk_norm_rope(rotary.c(hq, hk, d, dtype), n, *q_args, *k_args, None if positions is None else positions.data_ptr(), step, *q_to, *k_to, _stream(stream))
     if st:
@@ -281,8 +282,10 @@ _NO_ROWS = (None, 0, 0)
 
 def _on_device(device: int, *tensors):
     for t in tensors:
-        if t is not None and (t.get_device() != device or device < 0):
+        if t is not None and t.get_device() != device:
             raise ValueError("all tensors must be on one CUDA device")
+    if device < 0:
+        raise ValueError("all tensors must be on one CUDA device")
 
 
 def _rows(t, n: int, d: int, dtype):

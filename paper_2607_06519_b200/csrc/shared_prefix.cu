@@ -43,7 +43,7 @@ constexpr int kTok = 32;       // tokens at a time: a tile of the schedule
 constexpr int kThreads = 256;
 
 template <int D>
-constexpr int part_smem() { return (kRows * (D + 4) + 2 * kTok * (D + 4) + kRows * (kTok + 1) + 3 * kRows) * 4; }
+constexpr int part_smem() { return (kRows * (D + 4) + 2 * kTok * (D + 4) + kRows * (kTok + 1) + 2 * kRows) * 4; }
 
 // Tiles of kTok tokens are reconstructed into shared memory as float32 (rows, plus the sign times the scattered residual entries;
 // the unit's scale is applied to the logits and the outputs) and multiplied with the group's query rows: a thread has two rows x
@@ -58,72 +58,109 @@ __global__ void __launch_bounds__(kThreads) shared_part_kernel(SharedArgs a, con
     float* const sk = sq + kRows * P;
     float* const sv = sk + kTok * P;
     float* const sp = sv + kTok * P;             // [kRows][kTok + 1]
-    float* const sm = sp + kRows * (kTok + 1);   // maxima, sums, factors
+    float* const sm = sp + kRows * (kTok + 1);   // maxima, sums
     float* const sl = sm + kRows;
-    float* const sf = sl + kRows;
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;  // rows ty, ty + 16; tokens tx, tx + 16; channels 4 tx + 64 i
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // q belongs to the kernels ahead
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (behind the wait: the join reads the tails before its own)
     const int R = a.batch * a.G;
     const int range = blockIdx.x / sch.groups, group = blockIdx.x % sch.groups, row0 = group * kRows, rows = min(kRows, R - row0);
     int g0 = sch.start[range];
     const int g1 = sch.start[range + 1];
+    bool waited = false;
+    auto put8 = [&](float* to, const float (&f)[8]) {
+        *reinterpret_cast<float4*>(to) = make_float4(f[0], f[1], f[2], f[3]);
+        *reinterpret_cast<float4*>(to + 4) = make_float4(f[4], f[5], f[6], f[7]);
+    };
     while (g0 < g1) {
         const int h = g0 / sch.tiles, t_first = g0 % sch.tiles, t_last = min(sch.tiles, t_first + g1 - g0);
         g0 += t_last - t_first;
         const UnitDesc ud = a.desc[h];
         const bool resid = ud.mode == FDKV_MODE_RESIDUAL;
         const float kscale = ud.scale * rsqrtf((float)D), sign = ud.sign;
-        __syncthreads();
-        for (int i = tid; i < kRows * D / 8; i += kThreads) {
-            const int r = i / (D / 8), c = i % (D / 8) * 8;
-            float f[8] = {};
-            if (r < rows) {
-                const int row = row0 + r, b = row / a.G, g = row % a.G;
-                load8(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h * a.G + g) * D + c, f);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sq[r * P + c + j] = f[j];
-        }
-        if (tid < kRows) { sm[tid] = -INFINITY; sl[tid] = 0.f; }
         float o[2][D / 16];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) o[i][j] = 0.f;
         const int tok_end = min(ud.T, t_last * kTok);
+        constexpr int kPF = 2;
+        int next0[2] = {}, next1[2] = {};  // a tile's entries in either list
+        auto bounds = [&](int tok) {
+            const int s0 = tok / kResTile, s1 = (min(tok + kTok, tok_end) + kResTile - 1) / kResTile;
+            next0[0] = ud.k_off[s0];
+            next1[0] = ud.k_off[s1];
+            next0[1] = ud.v_off ? ud.v_off[s0] : next0[0];
+            next1[1] = ud.v_off ? ud.v_off[s1] : next1[0];
+        };
+        if (resid) bounds(t_first * kTok);
         for (int tok = t_first * kTok; tok < tok_end; tok += kTok) {
             const int n = min(kTok, tok_end - tok);
+            // the first entries of either list travel with the rows; the next tile's bounds are on their way meanwhile
+            int e0[2] = {next0[0], next0[1]}, e1[2] = {next1[0], next1[1]}, pi[2][kPF];
+            float pv[2][kPF];
+            if (resid) {
+                if (tok + kTok < tok_end) bounds(tok + kTok);
+                if (ud.res_kind != 1)
+#pragma unroll
+                    for (int l = 0; l < 2; ++l)
+#pragma unroll
+                        for (int k = 0; k < kPF; ++k) {
+                            const int e = e0[l] + tid + k * kThreads;
+                            if (e < e1[l]) {
+                                pi[l][k] = (l && ud.v_idx ? ud.v_idx : ud.k_idx)[e];
+                                pv[l][k] = ldf<T>(reinterpret_cast<const T*>(l ? ud.v_val : ud.k_val) + e);
+                            }
+                        }
+            }
             __syncthreads();
+#pragma unroll
             for (int i = tid; i < 2 * kTok * D / 8; i += kThreads) {
                 const bool is_v = i >= kTok * D / 8;
                 const int j = is_v ? i - kTok * D / 8 : i, t = j / (D / 8), c = j % (D / 8) * 8;
                 float f[8] = {};
                 if (t < n) load8(reinterpret_cast<const T*>(is_v ? ud.v_rows : ud.k_rows) + (int64_t)(tok + t) * D + c, f);
-                float* const to = (is_v ? sv : sk) + t * P + c;
-#pragma unroll
-                for (int x = 0; x < 8; ++x) to[x] = f[x];
+                put8((is_v ? sv : sk) + t * P + c, f);
             }
             __syncthreads();
             if (resid) {  // (every position is in a list once: no two threads add to the same place)
-                const int s0 = tok / kResTile, s1 = (tok + n + kResTile - 1) / kResTile;
+#pragma unroll
                 for (int is_v = 0; is_v < 2; ++is_v) {
-                    const int32_t* const off = is_v && ud.v_off ? ud.v_off : ud.k_off;
                     const int32_t* const idx = is_v && ud.v_idx ? ud.v_idx : ud.k_idx;
                     const T* const val = reinterpret_cast<const T*>(is_v ? ud.v_val : ud.k_val);
                     float* const to = is_v ? sv : sk;
-                    const int e0 = off[s0], e1 = off[s1];
                     if (ud.res_kind == 1) {  // whole rows of selected tokens
-                        for (int i = e0 * D + tid; i < e1 * D; i += kThreads) to[(idx[i / D] - tok) * P + i % D] += sign * ldf<T>(val + i);
+                        for (int i = e0[is_v] * D + tid; i < e1[is_v] * D; i += kThreads) to[(idx[i / D] - tok) * P + i % D] += sign * ldf<T>(val + i);
                     } else {
-                        for (int e = e0 + tid; e < e1; e += kThreads) {
+#pragma unroll
+                        for (int k = 0; k < kPF; ++k)
+                            if (e0[is_v] + tid + k * kThreads < e1[is_v]) {
+                                const int at = pi[is_v][k] - tok * D;
+                                to[at / D * P + at % D] += sign * pv[is_v][k];
+                            }
+                        for (int e = e0[is_v] + tid + kPF * kThreads; e < e1[is_v]; e += kThreads) {
                             const int at = idx[e] - tok * D;
                             to[at / D * P + at % D] += sign * ldf<T>(val + e);
                         }
                     }
                 }
-                __syncthreads();
             }
+            if (!waited) {  // (all so far is static since commit)
+                asm volatile("griddepcontrol.wait;" ::: "memory");               // q belongs to the kernels ahead
+                asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (behind the wait: the join reads the tails before its own)
+                waited = true;
+            }
+            if (tok == t_first * kTok) {
+                for (int i = tid; i < kRows * D / 8; i += kThreads) {
+                    const int r = i / (D / 8), c = i % (D / 8) * 8;
+                    float f[8] = {};
+                    if (r < rows) {
+                        const int row = row0 + r, b = row / a.G, g = row % a.G;
+                        load8(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h * a.G + g) * D + c, f);
+                    }
+                    put8(sq + r * P + c, f);
+                }
+                if (tid < kRows) { sm[tid] = -INFINITY; sl[tid] = 0.f; }
+            }
+            __syncthreads();
             // logits
             ACC s[2][2] = {};
 #pragma unroll 2
@@ -734,7 +771,8 @@ cudaError_t plan_shared_decode(const SharedArgs& a, int row_tile, int tile, int 
     int n_slow = 0;
     for (int h = 0; h < a.Hkv; ++h) n_slow += a.modes[h] == FDKV_MODE_RESIDUAL;
     const double f = (double)n_slow / a.Hkv, slow = kSlowTile + kSlowKept * a.keep, mean = sch.groups > 1 ? kGroupTile : kMeanTile;
-    const double plain = n_slow < a.Hkv ? std::max(kFastTile, (mean - f * slow) / (1.0 - f)) : mean, resid = slow / plain;
+    const double plain = n_slow < a.Hkv ? std::max(kFastTile, (mean - f * slow) / (1.0 - f)) : mean;
+    const double resid = tile == kSharedTile ? slow / plain : 1.0;  // (the portable kernel's blocks have a tile or two)
     double cost = 0.0;
     for (int h = 0; h < a.Hkv; ++h) cost += sch.tiles * (a.modes[h] == FDKV_MODE_RESIDUAL ? resid : 1.0);
     int h = 0;
