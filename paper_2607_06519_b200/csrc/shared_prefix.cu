@@ -743,8 +743,10 @@ cudaError_t launch_part(const SharedArgs& a, const SharedSched& sch, cudaStream_
 
 }  // namespace
 
-// us per tile of 128 tokens: with entries (and per kept fraction), without them when memory bounds all blocks, one or more row groups, and when it does not
-static constexpr double kSlowTile = 1.75, kSlowKept = 4.4, kMeanTile = 1.62, kGroupTile = 1.15, kFastTile = 1.0;
+// us per tile of 128 tokens: with entries (one or more row groups, and per kept fraction), without them when memory bounds all blocks (one or more row groups), and when it does
+// not.  Swept with half of the heads' tiles and more in each mode; us a call for equal tiles, 1.75, 1.9 and 2.1: 128k (1/32 kept, 16 sequences) 119.9, 108.1, 101.7 and 100.7, 32k
+// (1/16, eight) 38.1, 33.4, 32.9 and 32.1, (1/8) 45.6, 37.6, 36.1 and 35.6; two row groups, 32k: 69.1, 62.0, 63.3 and 65.8.
+static constexpr double kSlowTile = 2.1, kSlowGroupTile = 1.75, kSlowKept = 4.4, kMeanTile = 1.62, kGroupTile = 1.15, kFastTile = 1.0;
 // Whole tiles to the ranges, as evenly as their costs go.
 cudaError_t plan_shared_decode(const SharedArgs& a, int row_tile, int tile, int sms, SharedSched& sch) {
     const int R = a.batch * a.G;
@@ -770,7 +772,7 @@ cudaError_t plan_shared_decode(const SharedArgs& a, int row_tile, int tile, int 
     // less where blocks that are slower leave it room: that share of the time is what the others then take.
     int n_slow = 0;
     for (int h = 0; h < a.Hkv; ++h) n_slow += a.modes[h] == FDKV_MODE_RESIDUAL;
-    const double f = (double)n_slow / a.Hkv, slow = kSlowTile + kSlowKept * a.keep, mean = sch.groups > 1 ? kGroupTile : kMeanTile;
+    const double f = (double)n_slow / a.Hkv, slow = (sch.groups > 1 ? kSlowGroupTile : kSlowTile) + kSlowKept * a.keep, mean = sch.groups > 1 ? kGroupTile : kMeanTile;
     const double plain = n_slow < a.Hkv ? std::max(kFastTile, (mean - f * slow) / (1.0 - f)) : mean;
     const double resid = tile == kSharedTile ? slow / plain : 1.0;  // (the portable kernel's blocks have a tile or two)
     double cost = 0.0;

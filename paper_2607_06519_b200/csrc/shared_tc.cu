@@ -438,6 +438,10 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 const uint32_t ts = tq + cS + (it & 1) * 128;
                 mb_wait(sm0 + oS + 8 * (it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, a.status);
                 __syncwarp();
+                if (pair * 32 >= rows) {  // (no query has these rows: their scores, all zero, may stand for P)
+                    if (lane == 0) mb_arrive(sm0 + oP + 8 * (it & 1));
+                    continue;
+                }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 uint32_t s[2][32];
                 tmem_ld32(ts + 64 * half, s[0]);
