@@ -495,8 +495,10 @@ __device__ __forceinline__ float peer_load(uint32_t addr) {
 //   O^T[channel][head] += V^T P^T   a lane has eight channels of four tokens; a product's rows are channels eight apart
 // Up to four heads per group fill columns 0-3, columns 4-7 carry the remainder of P's rounding to bf16; eight heads take a second
 // product for it, so that P acts with 16 bits.  Blocks of a cluster share a unit's tail and parts (small batches, long tails).
-template <int G, int NB>
-__global__ void __launch_bounds__(kTcWarps * 32, 3) shared_join_tc_kernel(SharedArgs a, const __grid_constant__ SharedSched sch, const __grid_constant__ SharedSeqs<NB> sq) {
+// BLOCKS: on an SM at least.  Three keep all of a warp's registers; four, for more blocks than three have room for, keep more tail rows on their way
+// (32 768 and 2 048 tokens, 64 sequences of 200 tail tokens: 67.1 -> 64.8 and 27.3 -> 22.8 us; 32 sequences, which three hold, 17.3 and 19.7).
+template <int G, int NB, int BLOCKS>
+__global__ void __launch_bounds__(kTcWarps * 32, BLOCKS) shared_join_tc_kernel(SharedArgs a, const __grid_constant__ SharedSched sch, const __grid_constant__ SharedSeqs<NB> sq) {
     constexpr int D = 128, ITEMS = G * D / 4, THREADS = kTcWarps * 32;
     constexpr bool SPLIT = G <= 4;
     __shared__ __align__(16) float s_acc[kTcWarps][G][D];
@@ -562,7 +564,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, 3) shared_join_tc_kernel(Shared
                 mt[e] = fmaxf(p[0][e], p[1][e]);
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) mt[e] = fmaxf(mt[e], __shfl_xor_sync(0xFFFFFFFFu, mt[e], x));
-                const float mn = fmaxf(m[e], mt[e]), f = ex2(m[e] - mn);  // (finite: every step has a token)
+                const float mn = fmaxf(fmaxf(m[e], mt[e]), -1e30f), f = ex2(m[e] - mn);  // (finite, where every key so far is infinitely far off as well)
                 m[e] = mn;
                 l[e] *= f;
 #pragma unroll
@@ -707,6 +709,16 @@ template <typename T, int D>
 cudaError_t launch_join(const SharedArgs& a, const SharedSched& sch, cudaStream_t st) {
     return a.batch <= kSharedFew ? launch_join<T, D, kSharedFew>(a, sch, st) : launch_join<T, D, kMaxShared>(a, sch, st);
 }
+template <int NB, int BLOCKS>
+cudaError_t launch_join_tc(const cudaLaunchConfig_t& cfg, const SharedArgs& a, const SharedSched& sch, const SharedSeqs<NB>& sq) {
+    switch (a.G) {
+        case 1: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<1, NB, BLOCKS>, a, sch, sq);
+        case 2: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<2, NB, BLOCKS>, a, sch, sq);
+        case 4: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<4, NB, BLOCKS>, a, sch, sq);
+        case 8: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<8, NB, BLOCKS>, a, sch, sq);
+        default: return cudaErrorInvalidValue;
+    }
+}
 template <int NB>
 cudaError_t launch_join_tc(const SharedArgs& a, const SharedSched& sch, int sms, cudaStream_t st) {
     // blocks per unit: more than one while they leave half of the device idle and have parts or tail tokens for each
@@ -722,13 +734,7 @@ cudaError_t launch_join_tc(const SharedArgs& a, const SharedSched& sch, int sms,
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.numAttrs = ranks > 1 ? 2 : 1;
     const SharedSeqs<NB> sq = seqs_of<NB>(a);
-    switch (a.G) {
-        case 1: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<1, NB>, a, sch, sq);
-        case 2: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<2, NB>, a, sch, sq);
-        case 4: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<4, NB>, a, sch, sq);
-        case 8: return cudaLaunchKernelEx(&cfg, shared_join_tc_kernel<8, NB>, a, sch, sq);
-        default: return cudaErrorInvalidValue;
-    }
+    return a.Hkv * a.batch * ranks > 3 * sms ? launch_join_tc<NB, 4>(cfg, a, sch, sq) : launch_join_tc<NB, 3>(cfg, a, sch, sq);
 }
 
 template <typename T, int D>
