@@ -210,21 +210,19 @@ class Rotary:
         self._inv = (C.c_float * max(m, 1))(*[float(f) for f in inv_freq])
         self._axis = None if axis_of is None else (C.c_int32 * max(m, 1))(*[int(a) for a in axis_of])
         self.n_axes, self.q_weight, self.k_weight = n_axes, q_weight, k_weight
-        self._rows = None  # what the struct's sizes were set for
-        self._c = _Rotary(1, 1, 0, 0, 2 * m, int(interleaved), n_axes, eps, scale, C.addressof(self._inv),
-                          None if self._axis is None else C.addressof(self._axis),
-                          None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
+        self._rest = (2 * m, int(interleaved), n_axes, eps, scale, C.addressof(self._inv), None if self._axis is None else C.addressof(self._axis),
+                      None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
+        self._c = {}  # one struct for each set of sizes (a call reads it while other threads may make calls of other sizes)
 
     def c(self, n_q_heads: int, n_kv_heads: int, head_dim: int, tdtype) -> _Rotary:
         rows = (n_q_heads, n_kv_heads, head_dim, tdtype)
-        if rows != self._rows:
+        r = self._c.get(rows)
+        if r is None:
             for w in (self.q_weight, self.k_weight):
                 if w is not None and (w.dtype is not tdtype or len(w) != head_dim):
                     raise ValueError("norm weights must have the rows' dtype and head_dim")
-            r = self._c
-            r.n_q_heads, r.n_kv_heads, r.head_dim, r.dtype = n_q_heads, n_kv_heads, head_dim, _dtype_code(tdtype)
-            self._rows = rows
-        return self._c
+            r = self._c[rows] = _Rotary(n_q_heads, n_kv_heads, head_dim, _dtype_code(tdtype), *self._rest)
+        return r
 
 
 def _dtype_code(tdtype) -> int:
@@ -293,7 +291,7 @@ def _rows(t, n: int, d: int, dtype):
     tn, th, td = t.shape
     st, sh, sc = t.stride()
     if sc != 1 or tn != n or td != d or t.dtype is not dtype:
-        raise ValueError("queries and keys must be [n, heads, d] of one dtype, dense along d")
+        raise ValueError("rows must be [n, heads, d] of one dtype, dense along d")
     return t.data_ptr(), st if n > 1 else d, sh if th > 1 else d
 
 
@@ -406,11 +404,17 @@ class Context:
         seqs[b]; returns out [len(seqs), n_q_heads, d]."""
         od = self.cfg.dtype if out_dtype is None else out_dtype
         slots, n, _keep = _slots(seqs)
-        if len(q) != n:
-            raise ValueError("q needs one row per sequence")
+        c = self.cfg
+        if q.shape != (n, c.n_q_heads, c.head_dim) or q.dtype is not self.tdtype or not q.is_contiguous():
+            raise ValueError("q must be a contiguous [len(seqs), n_q_heads, head_dim] tensor of the context dtype")
+        for t in (k_new, v_new):
+            if t is not None and (t.shape != (n, c.n_kv_heads, c.head_dim) or t.dtype is not self.tdtype or not t.is_contiguous()):
+                raise ValueError("k_new and v_new must be contiguous [len(seqs), n_kv_heads, head_dim] tensors of the context dtype")
         _on_device(self.arena.get_device(), q, k_new, v_new, out)
-        if out is None:
-            out = torch.empty(q.shape, dtype=torch.bfloat16 if od == BF16 else torch.float32, device=self.device)
+        if self.arena.get_device() != torch._C._cuda_getDevice():
+            with torch.cuda.device(self.device):
+                return self.decode_attn_shared(layer, prompt_seq, seqs, q, k_new, v_new, out, out_dtype, stream)
+        out = self._out(out, n, od)
         st = _decode_attn_shared(self.h, layer, prompt_seq, slots, n, q.data_ptr(), None if k_new is None else k_new.data_ptr(),
                                  None if v_new is None else v_new.data_ptr(), out.data_ptr(), od, _stream(stream))
         if st:
@@ -431,21 +435,36 @@ class Context:
         if ns != n:
             raise ValueError("qkv needs one row per sequence")
         _on_device(self.arena.get_device(), qkv, positions, rotary.q_weight, rotary.k_weight, out)
-        if out is None:
-            out = torch.empty((n, c.n_q_heads, c.head_dim), dtype=torch.bfloat16 if od == BF16 else torch.float32, device=self.device)
+        if self.arena.get_device() != torch._C._cuda_getDevice():
+            with torch.cuda.device(self.device):
+                return self.decode_qkv(layer, rotary, qkv, positions, prompt_seq, seqs, out, out_dtype, stream)
+        out = self._out(out, n, od)
         _check(_lib.fdkv_decode_qkv(self.h, layer, prompt_seq, slots, n, rotary.c(c.n_q_heads, c.n_kv_heads, c.head_dim, self.tdtype), qkv.data_ptr(),
                                     qkv.stride(0) if n > 1 else qkv.shape[1], _ptr(positions), out.data_ptr(), od, _stream(stream)), "fdkv_decode_qkv")
         return out
 
     def append_tail(self, layer, seq, k, v, stream=None):
         """Appends rows k, v [n, n_kv_heads, d] (one strided layout) to a layer's tail of a sequence slot."""
-        if k.shape != v.shape or k.stride() != v.stride() or k.dtype is not self.tdtype or v.dtype is not self.tdtype or k.stride(2) != 1 or \
-                tuple(k.shape[1:]) != (self.cfg.n_kv_heads, self.cfg.head_dim):
-            raise ValueError("k and v must share one [n, Hkv, d] strided layout and the context dtype")
-        _on_device(self.arena.get_device(), k, v)
         n, d = len(k), self.cfg.head_dim
-        _check(_lib.fdkv_append_tail(self.h, layer, seq, n, _ptr(k), _ptr(v), k.stride(0) if n > 1 else d, k.stride(1) if k.shape[1] > 1 else d, _stream(stream)),
-               "fdkv_append_tail")
+        if k.shape != v.shape or tuple(k.shape[1:]) != (self.cfg.n_kv_heads, d):
+            raise ValueError("k and v must be [n, Hkv, d]")
+        kp, *strides = _rows(k, n, d, self.tdtype)
+        vp, *of_v = _rows(v, n, d, self.tdtype)
+        if strides != of_v:
+            raise ValueError("k and v must share one strided layout")
+        _on_device(self.arena.get_device(), k, v)
+        with torch.cuda.device(self.device):
+            _check(_lib.fdkv_append_tail(self.h, layer, seq, n, kp, vp, *strides, _stream(stream)), "fdkv_append_tail")
+
+    def _out(self, out, n, out_dtype):
+        """The attention's output tensor, or a new one; a caller's is checked."""
+        tdtype = torch.bfloat16 if out_dtype == BF16 else torch.float32
+        shape = (n, self.cfg.n_q_heads, self.cfg.head_dim)
+        if out is None:
+            return torch.empty(shape, dtype=tdtype, device=self.device)
+        if out.dtype is not tdtype or out.numel() != n * shape[1] * shape[2] or not out.is_contiguous():
+            raise ValueError("out must be a contiguous [len(seqs), n_q_heads, head_dim] tensor of the output type")
+        return out
 
     def decode_attn_host(self, layer, q, k_new, v_new, out, out_dtype, stream=None):
         """Same with host (ideally pinned) tensors; synchronous."""

@@ -20,7 +20,7 @@ class Prompt:
     """A context whose slot `slot` holds a committed prompt of one block of layers, and the rows of every layer in float64."""
 
     def __init__(self, T, G, hkv, d, dtype, block=2, rule=0, keep=(1, 8), modes=None, max_batch=4, max_tail=300, slot=0, seed=0, max_fold=0, row_format=0,
-                 max_prefill=None, device="cuda:0"):
+                 max_prefill=None, device="cuda:0", kv=None):
         from paper_2607_06519_b200 import binding as B
 
         self.B, self.T, self.G, self.hkv, self.d, self.dtype, self.slot, self.block = B, T, G, hkv, d, dtype, slot, block
@@ -28,7 +28,7 @@ class Prompt:
                        row_format)
         self.ctx = B.Context(cfg, device=device)
         g = self.g = torch.Generator(device="cuda").manual_seed(seed)
-        self.k, self.v = chain(g, T, hkv, d, block, dtype), chain(g, T, hkv, d, block, dtype)
+        self.k, self.v = kv or (chain(g, T, hkv, d, block, dtype), chain(g, T, hkv, d, block, dtype))
         self.modes = [h % 3 for h in range(hkv)] if modes is None else modes
         ctx = self.ctx
         ctx.compress_prefill(slot, 0, 1, T, self.k, self.v)

@@ -179,6 +179,133 @@ def test_append_tail_before_an_ordinary_decode_step(dtype, d):
     p.close()
 
 
+@pytest.mark.parametrize("batch,hkv,G,tail", [(80, 6, 4, 90), (150, 3, 8, 40), (2, 2, 4, 2500), (1, 1, 8, 1100), (3, 8, 1, 700)])
+def test_joins_of_many_units_and_of_long_tails(batch, hkv, G, tail):
+    """More blocks than three on every SM; clusters of two to eight blocks that share a unit's tail and outputs."""
+    p = Prompt(1500, G, hkv, 128, BF, max_batch=batch, max_tail=tail + 1, modes=[h % 3 for h in range(hkv)], seed=batch)
+    lens = [max(0, tail - 7 * b) for b in range(batch)]
+    tails = random_tails(p, lens)
+    put_tails(p, 0, list(range(batch)), tails)
+    for _ in range(2):
+        q, kn, vn = p.new(batch, G * hkv, 128), p.new(batch, hkv, 128), p.new(batch, hkv, 128)
+        if lens[0] < tail + 1:
+            tails = [(torch.cat([k, kn[b:b + 1]]), torch.cat([v, vn[b:b + 1]])) for b, (k, v) in enumerate(tails)]
+            out = p.ctx.decode_attn_shared(0, 0, list(range(batch)), q, kn, vn)
+            lens[0] += 1
+        else:
+            out = p.ctx.decode_attn_shared(0, 0, list(range(batch)), q)
+        p.check(out, 0, q, tails)
+    p.close()
+
+
+@pytest.mark.parametrize("dtype,d,G", [(BF, 128, 4), (BF, 128, 8), (F, 64, 2), (BF, 64, 1)])
+def test_tail_rows_infinitely_far_off(dtype, d, G):
+    """Keys whose logit is minus infinity: their tokens count for nothing, also where a sequence has no others, or a warp's first ones are such."""
+    p = Prompt(200, G, 2, d, dtype, seed=40)
+    lens, off = [1, 70, 300], [1, 65, 299]
+    tails = random_tails(p, lens)
+    for (k, _), m in zip(tails, off):
+        k[:m, :, 0] = float("-inf")
+    put_tails(p, 0, [0, 1, 2], tails)
+    q = p.new(3, 2 * G, d)
+    q[:, :, 0] = q[:, :, 0].abs() + 1
+    out = p.ctx.decode_attn_shared(0, 0, [0, 1, 2], q)
+    p.check(out, 0, q, [(k[m:], v[m:]) for (k, v), m in zip(tails, off)])
+    p.close()
+
+
+def test_refused_tensors():
+    """Sizes, types and strides that the call would read past or misread."""
+    p = Prompt(64, 2, 2, 64, F, seed=41)
+    q, kn = p.new(2, 4, 64), p.new(2, 2, 64)
+    for bad in (dict(q=p.new(2, 3, 64)), dict(q=q.to(BF)), dict(q=p.new(2, 64, 4).mT), dict(q=q.flatten(1)), dict(k=p.new(2, 1, 64)), dict(v=kn.to(BF)),
+                dict(k=p.new(1, 2, 64)), dict(v=p.new(2, 64, 2).mT), dict(out=torch.empty_like(q[:1])), dict(out=q.to(BF)), dict(out=p.new(2, 64, 4).mT)):
+        with pytest.raises(ValueError):
+            p.ctx.decode_attn_shared(0, 0, [0, 1], bad.get("q", q), bad.get("k", kn), bad.get("v", kn), out=bad.get("out"))
+    r = p.B.Rotary([])
+    with pytest.raises(ValueError):
+        p.ctx.decode_qkv(0, r, p.new(2, 8 * 64), None, 0, [0, 1], out=torch.empty_like(q[:1]))
+    for k, v in ((kn, kn[:1]), (kn, kn.to(BF)), (p.new(2, 1, 64), p.new(2, 1, 64)), (kn, p.new(2, 4, 64)[:, ::2]), (p.new(2, 64, 2).mT, p.new(2, 64, 2).mT)):
+        with pytest.raises(ValueError):
+            p.ctx.append_tail(0, 1, k, v)
+    p.check(p.ctx.decode_attn_shared(0, 0, [0, 1], q), 0, q, random_tails(p, [0, 0]))  # nothing was appended
+    p.close()
+
+
+def test_one_rotation_for_calls_of_several_sizes():
+    from paper_2607_06519_b200 import binding as B
+
+    r = B.Rotary([1.0] * 32, scale=2.0)
+    pos = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for hq, hk, d, dtype in ((4, 2, 64, F), (1, 1, 128, BF), (4, 2, 64, F)):
+        q, k = torch.randn((3, hq, d), device="cuda").to(dtype), torch.randn((3, hk, d), device="cuda").to(dtype)
+        for a, b in ((q, k), (q, None), (None, k)):
+            for x, y in zip((a, b), B.qk_norm_rope(r, a, b, pos)):
+                assert (x is None) == (y is None)
+                if x is not None:
+                    assert torch.equal(y[..., :64], 2 * x[..., :64]) and torch.equal(y[..., 64:], x[..., 64:])
+
+
+def test_which_kernel_serves():
+    from paper_2607_06519_b200 import binding as B
+
+    for dtype, d, kernel in ((BF, 128, B.KERNEL_SHARED_TC), (F, 128, B.KERNEL_SHARED_PORTABLE), (BF, 64, B.KERNEL_SHARED_PORTABLE)):
+        p = Prompt(200, 2, 2, d, dtype, seed=1)
+        before = [B.kernel_launch_count(k) for k in (B.KERNEL_SHARED_TC, B.KERNEL_SHARED_PORTABLE)]
+        p.ctx.decode_attn_shared(0, 0, [1], p.new(1, 4, d))
+        after = [B.kernel_launch_count(k) for k in (B.KERNEL_SHARED_TC, B.KERNEL_SHARED_PORTABLE)]
+        assert [b - a for a, b in zip(before, after)] == [int(kernel == B.KERNEL_SHARED_TC), int(kernel == B.KERNEL_SHARED_PORTABLE)]
+        p.close()
+
+
+@pytest.mark.parametrize("rule,block", [(0, 2), (1, 4)])
+def test_a_prompt_and_its_continuations(rule, block):
+    """All of it as a serving program has it: a prompt's projection rows are normed and rotated into the layers' rows, compressed, probed and committed; every
+    sequence's own question goes behind it in bulk; then steps from fused rows, each layer of each step against 64 bits."""
+    from paper_2607_06519_b200 import binding as B
+
+    T, G, hkv, d, n = 700, 4, 2, 128, 5
+    hq = G * hkv
+    g = torch.Generator(device="cuda").manual_seed(31)
+    inv = [10000.0 ** (-2.0 * i / d) for i in range(d // 2)]
+    axis = [i % 3 for i in range(d // 2)]
+    rot = [B.Rotary(inv, axis_of=axis, n_axes=3, q_weight=torch.ones(d, device="cuda", dtype=BF) * (1 + 0.1 * l), k_weight=torch.ones(d, device="cuda", dtype=BF))
+           for l in range(block)]
+
+    def projected(rows):
+        return torch.randn((rows, hq + 2 * hkv, d), generator=g, device="cuda").to(BF)
+
+    def positions(start, rows):
+        return torch.stack([start + torch.arange(rows, device="cuda") // s for s in (1, 3, 7)]).to(torch.int32)
+
+    k, v, q_last = [], [], []
+    for l in range(block):
+        x = projected(T)
+        rows = torch.zeros((T, hkv, d), device="cuda", dtype=BF)
+        q, _ = B.qk_norm_rope(rot[l], x[:, :hq], x[:, hq:hq + hkv], positions(0, T), k_out=rows)
+        k.append(rows)
+        v.append(x[:, hq + hkv:].contiguous())
+        q_last.append(q[-8:].contiguous())
+    p = Prompt(T, G, hkv, d, BF, block=block, rule=rule, max_batch=n, max_tail=40, modes=[1, 0], seed=32, kv=(k, v))
+    tails = [[None] * n for _ in range(block)]
+    for l in range(block):
+        for b in range(n):
+            m = 3 * b + 1
+            x = projected(m)
+            _, own = B.qk_norm_rope(rot[l], None, x[:, hq:hq + hkv], positions(T, m))
+            p.ctx.append_tail(l, b, own, x[:, hq + hkv:].contiguous())
+            tails[l][b] = (own, x[:, hq + hkv:])
+    for step in range(3):
+        for l in range(block):
+            x = projected(n)
+            pos = torch.stack([torch.tensor([T + 3 * b + 1 + step for b in range(n)], device="cuda")] * 3).to(torch.int32)
+            q, kn = B.qk_norm_rope(rot[l], x[:, :hq], x[:, hq:hq + hkv], pos)
+            tails[l] = [(torch.cat([a, kn[b:b + 1]]), torch.cat([c, x[b:b + 1, hq + hkv:]])) for b, (a, c) in enumerate(tails[l])]
+            out = p.ctx.decode_qkv(l, rot[l], x.view(n, -1), pos, 0, list(range(n)))
+            p.check(out, l, q, tails[l])
+    p.close()
+
+
 def test_streams_and_captured_calls():
     p = Prompt(3000, 4, 2, 128, BF, max_batch=4, seed=13)
     seqs, lens = [1, 2, 3], [9, 0, 140]
