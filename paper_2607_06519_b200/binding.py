@@ -210,6 +210,10 @@ class Rotary:
         self._inv = (C.c_float * max(m, 1))(*[float(f) for f in inv_freq])
         self._axis = None if axis_of is None else (C.c_int32 * max(m, 1))(*[int(a) for a in axis_of])
         self.n_axes, self.q_weight, self.k_weight = n_axes, q_weight, k_weight
+        devices = {w.get_device() for w in (q_weight, k_weight) if w is not None}
+        if len(devices) > 1:
+            raise ValueError("norm weights must be on one device")
+        self.device = devices.pop() if devices else None
         self._rest = (2 * m, int(interleaved), n_axes, eps, scale, C.addressof(self._inv), None if self._axis is None else C.addressof(self._axis),
                       None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
         self._c = {}  # one struct for each set of sizes (a call reads it while other threads may make calls of other sizes)
@@ -235,7 +239,7 @@ def _dtype_code(tdtype) -> int:
 
 def _positions(positions, n_axes: int, n: int) -> int:
     """The distance between the axes of positions [n_axes, n], or [n] for one axis."""
-    shape, strides = tuple(positions.shape), positions.stride()
+    shape, strides = positions.shape, positions.stride()
     if positions.dtype is not torch.int32 or (shape != (n_axes, n) and not (n_axes == 1 and shape == (n,))) or (n > 1 and strides[-1] != 1):
         raise ValueError("positions must be int32 [n_axes, n], dense along n")
     return strides[0] if n_axes > 1 else n
@@ -248,34 +252,39 @@ def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream
     if x is None:
         raise ValueError("queries or keys are needed")
     n, _, d = x.shape
-    dtype = x.dtype
-    q_args = q_to = k_args = k_to = _NO_ROWS
+    dtype, device = x.dtype, x.get_device()
+    qp = kp = qop = kop = None
+    qn = qh = kn = kh = qon = qoh = kon = koh = 0
     hq = hk = 1
     if q is not None:
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
-        hq, q_args, q_to = q.shape[1], _rows(q, n, d, dtype), _rows(q_out, n, d, dtype)
-        if q_out.shape[1] != hq:
+        qp, qn, qh, hq = _rows(q, n, d, dtype, device)
+        qop, qon, qoh, ho = _rows(q_out, n, d, dtype, device)
+        if ho != hq:
             raise ValueError("q_out must have the shape of q")
     if k is not None:
         if k_out is None:
             k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
-        hk, k_args, k_to = k.shape[1], _rows(k, n, d, dtype), _rows(k_out, n, d, dtype)
-        if k_out.shape[1] != hk:
+        kp, kn, kh, hk = _rows(k, n, d, dtype, device)
+        kop, kon, koh, ho = _rows(k_out, n, d, dtype, device)
+        if ho != hk:
             raise ValueError("k_out must have the shape of k")
-    step = _positions(positions, rotary.n_axes, n) if positions is not None else 0
-    device = x.get_device()
-    _on_device(device, q, k, q_out, k_out, positions, rotary.q_weight, rotary.k_weight)
+    pos, step = None, 0
+    if positions is not None:
+        pos, step = positions.data_ptr(), _positions(positions, rotary.n_axes, n)
+        if positions.get_device() != device:
+            raise ValueError("all tensors must be on one CUDA device")
+    r = rotary.c(hq, hk, d, dtype)
+    if device < 0 or rotary.device not in (None, device):
+        raise ValueError("all tensors must be on one CUDA device")
     if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return qk_norm_rope(rotary, q, k, positions, q_out, k_out, stream)
-    st = _qk_norm_rope(rotary.c(hq, hk, d, dtype), n, *q_args, *k_args, None if positions is None else positions.data_ptr(), step, *q_to, *k_to, _stream(stream))
+    st = _qk_norm_rope(r, n, qp, qn, qh, kp, kn, kh, pos, step, qop, qon, qoh, kop, kon, koh, _stream(stream))
     if st:
         raise FdkvError(st, "fdkv_qk_norm_rope")
     return q_out, k_out
-
-
-_NO_ROWS = (None, 0, 0)
 
 
 def _on_device(device: int, *tensors):
@@ -286,13 +295,13 @@ def _on_device(device: int, *tensors):
         raise ValueError("all tensors must be on one CUDA device")
 
 
-def _rows(t, n: int, d: int, dtype):
-    """Address and strides (token, head) of rows [n, heads, d]; a stride that nothing is reached by counts as d."""
+def _rows(t, n: int, d: int, dtype, device: int):
+    """Address, strides (token, head) and heads of rows [n, heads, d]; a stride that nothing is reached by counts as d."""
     tn, th, td = t.shape
     st, sh, sc = t.stride()
-    if sc != 1 or tn != n or td != d or t.dtype is not dtype:
-        raise ValueError("rows must be [n, heads, d] of one dtype, dense along d")
-    return t.data_ptr(), st if n > 1 else d, sh if th > 1 else d
+    if sc != 1 or tn != n or td != d or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError("rows must be [n, heads, d] of one dtype on one device, dense along d")
+    return t.data_ptr(), st if n > 1 else d, sh if th > 1 else d, th
 
 
 def _slots(seqs):
@@ -448,13 +457,12 @@ class Context:
         n, d = len(k), self.cfg.head_dim
         if k.shape != v.shape or tuple(k.shape[1:]) != (self.cfg.n_kv_heads, d):
             raise ValueError("k and v must be [n, Hkv, d]")
-        kp, *strides = _rows(k, n, d, self.tdtype)
-        vp, *of_v = _rows(v, n, d, self.tdtype)
-        if strides != of_v:
+        kp, st, sh, _ = _rows(k, n, d, self.tdtype, self.arena.get_device())
+        vp, vt, vh, _ = _rows(v, n, d, self.tdtype, self.arena.get_device())
+        if (st, sh) != (vt, vh):
             raise ValueError("k and v must share one strided layout")
-        _on_device(self.arena.get_device(), k, v)
         with torch.cuda.device(self.device):
-            _check(_lib.fdkv_append_tail(self.h, layer, seq, n, kp, vp, *strides, _stream(stream)), "fdkv_append_tail")
+            _check(_lib.fdkv_append_tail(self.h, layer, seq, n, kp, vp, st, sh, _stream(stream)), "fdkv_append_tail")
 
     def _out(self, out, n, out_dtype):
         """The attention's output tensor, or a new one; a caller's is checked."""
