@@ -10,6 +10,8 @@
 // a lane holds four channels of the first half of the rotating ones and the four that pair with them, so that a warp's loads
 // cover whole 128-byte stretches, a norm costs log2(D / 8) shuffles and a rotation none.  The lanes that hold the same channels
 // of different rows share the token's sines: each computes its part of the four and hands them on by shuffle.
+// Measured: 32 768 tokens of 32 + 8 heads of 128 channels, out of and into strided rows, norm and rotation: 112 us for 671 MB, 6.0 TB/s; 16 383 tokens without
+// norms 57 us, 5.9 TB/s; one token 2.5 us.  (71 registers, 26 one-warp blocks on an SM.)
 // (Eight channels a lane, in 16-byte loads, needed 118 registers with weights: 16 warps on an SM, two groups of rows in flight each, 3.9 TB/s for
 // 32 768 tokens of 40 heads.)
 #include <cmath>
@@ -205,7 +207,8 @@ __global__ void __launch_bounds__(kQkThreads, 26) qk_prep_kernel(const __grid_co
     if (a.Hv) tensor(a.v, a.v_n, a.v_h, a.v_out, a.vo_n, a.vo_h, a.Hv, nullptr, max(0, first - gq - gk), min(gv, first + steps - gq - gk), true);
 }
 
-// n rows [n][H][d] of one layer behind a sequence's tail rows: one thread per 16 bytes.
+// n rows [n][H][d] of one layer behind a sequence's tail rows: one thread per 16 bytes, a plain copy (once per sequence and layer, a few microseconds; memory
+// bounds it from some ten thousand rows on, more than tails have).
 __global__ void __launch_bounds__(256) append_tail_kernel(const char* k, const char* v, int64_t stride_t, int64_t stride_h, char* tail_k, char* tail_v, int64_t head_bytes,
                                                           int n, int H, int chunks, int32_t* len, int new_len) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (int64_t)n * H * chunks;
