@@ -554,6 +554,13 @@ __global__ void __launch_bounds__(kTcWarps * 32, BLOCKS) shared_join_tc_kernel(S
                 v[i][0] = __ldcg(reinterpret_cast<const uint4*>(p));
                 v[i][1] = __ldcg(reinterpret_cast<const uint4*>(p + 64));
             }
+            if (t0 + step < n) {  // the next step's rows, one a lane, on their way to L2 (behind the last one nothing is asked for)
+                const int t = t0 + step + (lane & 15);
+                if (t < n) {
+                    const __nv_bfloat16* const p = (lane < 16 ? tk : tv) + (int64_t)t * D;
+                    asm volatile("prefetch.global.L2 [%0];\n\tprefetch.global.L2 [%0 + 128];" ::"l"(p));
+                }
+            }
             float s[2][4] = {};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
