@@ -497,8 +497,8 @@ __device__ __forceinline__ float peer_load(uint32_t addr) {
 //   O^T[channel][head] += V^T P^T   a lane has eight channels of four tokens; a product's rows are channels eight apart
 // Up to four heads per group fill columns 0-3, columns 4-7 carry the remainder of P's rounding to bf16; eight heads take a second
 // product for it, so that P acts with 16 bits.  Blocks of a cluster share a unit's tail and parts (small batches, long tails).
-// Bound by the loads a warp has on their way: 64 sequences of 200 tokens are 52 MB of tails, 12 us of a call (8 at the copy rate); for small batches by the chain parts ->
-// sums -> outputs behind the prompt kernel, 2 to 3 us of which ten parts at a time hide the most.
+// Bound by memory and the loads on their way: 64 sequences of 200 tokens are 52 MB of tails, 10 us of a call (8 at the copy rate), of 1 000 262 MB, 50 us; for small
+// batches by the chain parts -> sums -> outputs behind the prompt kernel, with ten parts on their way at a time.
 // BLOCKS: on an SM at least.  Three keep all of a warp's registers; four, for more blocks than three have room for, keep more tail rows on their way
 // (32 768 and 2 048 tokens, 64 sequences of 200 tail tokens: 67.1 -> 64.8 and 27.3 -> 22.8 us; 32 sequences, which three hold, 17.3 and 19.7).
 template <int G, int NB, int BLOCKS>
@@ -554,7 +554,9 @@ __global__ void __launch_bounds__(kTcWarps * 32, BLOCKS) shared_join_tc_kernel(S
                 v[i][0] = __ldcg(reinterpret_cast<const uint4*>(p));
                 v[i][1] = __ldcg(reinterpret_cast<const uint4*>(p + 64));
             }
-            if (t0 + step < n) {  // the next step's rows, one a lane, on their way to L2 (behind the last one nothing is asked for)
+            // The next step's rows, one a lane, on their way to L2 (64 sequences of 1 000 own tokens: 82.9 -> 62.0 us; two steps ahead 67.5, both
+            // 69.8; of 200, 22.6 -> 23.5 behind 2 048 tokens and 64.6 -> 62.4 behind 32 768).
+            if (t0 + step < n) {
                 const int t = t0 + step + (lane & 15);
                 if (t < n) {
                     const __nv_bfloat16* const p = (lane < 16 ? tk : tv) + (int64_t)t * D;
