@@ -258,14 +258,14 @@ def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream
     hq = hk = 1
     if q is not None:
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+            q_out = _empty(q.shape, dtype, q.device, stream)
         qp, qn, qh, hq = _rows(q, n, d, dtype, device)
         qop, qon, qoh, ho = _rows(q_out, n, d, dtype, device)
         if ho != hq:
             raise ValueError("q_out must have the shape of q")
     if k is not None:
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
+            k_out = _empty(k.shape, dtype, k.device, stream)
         kp, kn, kh, hk = _rows(k, n, d, dtype, device)
         kop, kon, koh, ho = _rows(k_out, n, d, dtype, device)
         if ho != hk:
@@ -285,6 +285,14 @@ def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream
     if st:
         raise FdkvError(st, "fdkv_qk_norm_rope")
     return q_out, k_out
+
+
+def _empty(shape, dtype, device, stream):
+    """A new output; it belongs to the stream that writes it, so that its memory is not handed out on another one while that does."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _on_device(device: int, *tensors):
@@ -423,7 +431,7 @@ class Context:
         if self.arena.get_device() != torch._C._cuda_getDevice():
             with torch.cuda.device(self.device):
                 return self.decode_attn_shared(layer, prompt_seq, seqs, q, k_new, v_new, out, out_dtype, stream)
-        out = self._out(out, n, od)
+        out = self._out(out, n, od, stream)
         st = _decode_attn_shared(self.h, layer, prompt_seq, slots, n, q.data_ptr(), None if k_new is None else k_new.data_ptr(),
                                  None if v_new is None else v_new.data_ptr(), out.data_ptr(), od, _stream(stream))
         if st:
@@ -447,7 +455,7 @@ class Context:
         if self.arena.get_device() != torch._C._cuda_getDevice():
             with torch.cuda.device(self.device):
                 return self.decode_qkv(layer, rotary, qkv, positions, prompt_seq, seqs, out, out_dtype, stream)
-        out = self._out(out, n, od)
+        out = self._out(out, n, od, stream)
         _check(_lib.fdkv_decode_qkv(self.h, layer, prompt_seq, slots, n, rotary.c(c.n_q_heads, c.n_kv_heads, c.head_dim, self.tdtype), qkv.data_ptr(),
                                     qkv.stride(0) if n > 1 else qkv.shape[1], _ptr(positions), out.data_ptr(), od, _stream(stream)), "fdkv_decode_qkv")
         return out
@@ -464,12 +472,12 @@ class Context:
         with torch.cuda.device(self.device):
             _check(_lib.fdkv_append_tail(self.h, layer, seq, n, kp, vp, st, sh, _stream(stream)), "fdkv_append_tail")
 
-    def _out(self, out, n, out_dtype):
+    def _out(self, out, n, out_dtype, stream):
         """The attention's output tensor, or a new one; a caller's is checked."""
         tdtype = torch.bfloat16 if out_dtype == BF16 else torch.float32
         shape = (n, self.cfg.n_q_heads, self.cfg.head_dim)
         if out is None:
-            return torch.empty(shape, dtype=tdtype, device=self.device)
+            return _empty(shape, tdtype, self.device, stream)
         if out.dtype is not tdtype or out.numel() != n * shape[1] * shape[2] or not out.is_contiguous():
             raise ValueError("out must be a contiguous [len(seqs), n_q_heads, head_dim] tensor of the output type")
         return out

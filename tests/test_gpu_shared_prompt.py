@@ -232,6 +232,27 @@ def test_refused_tensors():
     p.close()
 
 
+def test_new_outputs_belong_to_the_stream_that_writes_them():
+    from paper_2607_06519_b200 import binding as B
+
+    p = Prompt(300, 4, 2, 64, F, seed=42)
+    side = torch.cuda.Stream()
+    q, pos, r = p.new(2, 8, 64), torch.zeros(2, dtype=torch.int32, device="cuda"), B.Rotary([1.0] * 32)
+    row = p.new(2, 12 * 64)
+    torch.cuda.synchronize()
+    calls = (lambda: p.ctx.decode_attn_shared(0, 0, [0, 1], q, stream=side), lambda: B.qk_norm_rope(r, q, None, pos, stream=side)[0],
+             lambda: B.qk_norm_rope(r, None, q, pos, stream=side)[1], lambda: p.ctx.decode_qkv(0, r, row, pos, 0, [2, 3], stream=side))
+    for call in calls:
+        out = call()
+        at = out.data_ptr()
+        del out  # (what frees it does not wait for the side stream)
+        assert all(torch.empty((2, 8, 64), device="cuda").data_ptr() != at for _ in range(3))
+    out = calls[0]()
+    torch.cuda.synchronize()
+    p.check(out, 0, q, random_tails(p, [0, 0]))
+    p.close()
+
+
 def test_one_rotation_for_calls_of_several_sizes():
     from paper_2607_06519_b200 import binding as B
 
