@@ -239,6 +239,7 @@ fdkv_status fdkv_decode_step_host(fdkv_ctx* ctx, int32_t batch, const void* q /*
  * committed at the time of the call: after fdkv_fold_tail on it, the folded tokens belong to it for every sequence.
  * bf16 storage with head_dim 128: the prompt's probabilities are rounded to bf16 for the second product (float32 sums), so that out is
  * within about 1e-3 of the exact attention before its own rounding; the rest in float32 (1e-6).  FDKV_ROWS_E4M3 contexts: FDKV_ERR_UNSUPPORTED.
+ * A query whose logits are all minus infinity gets zeros.
  * Like fdkv_decode_attn's, a call's split-K parts lie in the workspace: calls of one context on several streams, replays of
  * captured ones among them, are ordered by the caller.
  */

@@ -573,11 +573,11 @@ __global__ void __launch_bounds__(kTcWarps * 32, BLOCKS) shared_join_tc_kernel(S
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) p[i][e] = t0 + gid + 8 * i < n ? (s[0][2 * i + e] + s[1][2 * i + e]) * ks : -INFINITY;
+                for (int i = 0; i < 2; ++i) p[i][e] = t0 + gid + 8 * i < n ? __fmul_rn(s[0][2 * i + e] + s[1][2 * i + e], ks) : -INFINITY;
                 mt[e] = fmaxf(p[0][e], p[1][e]);
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) mt[e] = fmaxf(mt[e], __shfl_xor_sync(0xFFFFFFFFu, mt[e], x));
-                const float mn = fmaxf(fmaxf(m[e], mt[e]), -1e30f), f = ex2(m[e] - mn);  // (finite, where every key so far is infinitely far off as well)
+                const float mn = fmaxf(fmaxf(m[e], mt[e]), -1e38f), f = ex2(m[e] - mn);  // (finite where every key so far is infinitely far off, and below all finite scores)
                 m[e] = mn;
                 l[e] *= f;
 #pragma unroll

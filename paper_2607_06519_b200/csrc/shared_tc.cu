@@ -35,6 +35,12 @@ namespace {
 constexpr int kThreads = 640;  // five warpgroups; the last one's warps 18 and 19 have nothing to do
 constexpr int kSlots = 7, kSlotBytes = 32768, kHalf = 16384;
 constexpr float kLazy = 16.f;  // (powers of two)
+// The exponents' reference while a row has met no finite score: below all of those (float32's lowest / sqrt(128), in powers of two, is -4.4e37) and finite itself,
+// so that the exponential of a score of minus infinity is zero, not that of a NaN.
+constexpr float kFloor = -1e38f;
+// s * ks - m in one rounding differs from the rounded products, of which m is one, by up to 2^-24 |m|.  Beyond this reference, where neighbouring scores are
+// 16 powers of two apart, a power of two takes the place of ks, so that the largest score's difference is zero.
+constexpr float kFar = 134217728.f;
 constexpr int kHeader = 1024, kOnes = 2048;  // (16 rows of 128 bytes, bf16 ones)
 constexpr int kSmem = kHeader + kOnes + kSlots * kSlotBytes;
 static_assert(kSmem <= 227 * 1024, "shared memory budget");
@@ -410,23 +416,40 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 __syncwarp();
                 if (lane == 0) mb_arrive(sm0 + oQ);
             }
-            float m = -INFINITY;  // what the exponents are relative to, in powers of two: the same for both halves
+            // A score's exponent is score * scale + shift: ks and minus the reference m (in powers of two, the same for both halves), or, far off, the
+            // power of two below ks and what makes the reference's exponent zero.
+            const float two = __uint_as_float(__float_as_uint(ks) & 0x7F800000u);
+            float scale = two, shift = -kFloor;
+            auto reference = [&]() { return scale == ks ? -shift : fmaxf(-shift / scale * ks, kFloor); };
+            auto set_reference = [&](float raw) {
+                const float m = fmaxf(raw * ks, kFloor);
+                scale = fabsf(m) > kFar ? two : ks;
+                shift = fabsf(m) > kFar ? fminf(-raw * two, -kFloor) : -m;
+            };
             // A score of the warps' rows passes the reference by more than 2^kLazy (or there is none yet): both halves take the larger of their
-            // maxima, and each scales its half of the accumulators down, by a power of two.
-            auto move_reference = [&](float top, int j) {
-                tmem_st1(tq + cX + half, __float_as_uint(top));
+            // maxima, and each scales its half of the accumulators down, by a power of two.  From or to a reference far off (rows whose scores so far were
+            // the lowest values) the steps would be rounded, and it is set anew.
+            auto move_reference = [&](float raw, int j) {
+                tmem_st1(tq + cX + half, __float_as_uint(raw));
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 pair_sync(pair);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                top = fmaxf(top, __uint_as_float(tmem_ld1(tq + cX + (half ^ 1))));
+                raw = fmaxf(raw, __uint_as_float(tmem_ld1(tq + cX + (half ^ 1))));
                 // (the other half has read this one's before either comes here again: the barrier of the next tile lies between)
                 if (j == 0) {
-                    m = top;
+                    set_reference(raw);
                     return;
                 }
-                const float up = fmaxf(0.f, ceilf(top - m)), f = ex2(-up);
-                m += up;
+                const float m = reference(), up = fmaxf(0.f, ceilf(raw * ks - m));
+                float f = 1.f;
+                if (up < 200.f && scale == ks) {
+                    f = ex2((shift - up) - shift);  // (the step as it is rounded)
+                    shift -= up;
+                } else if (up > 0.f) {
+                    f = ex2(m - raw * ks);
+                    set_reference(raw);
+                }
                 mb_wait(sm0 + oO + 8 * ((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u, abort_flag, a.status);
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -470,17 +493,17 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                     for (int i = 2; i < 16; i += 2)
                         mx[k] = fmaxf(fmaxf(mx[k], __uint_as_float(s[k & 1][16 * (k >> 1) + i])), __uint_as_float(s[k & 1][16 * (k >> 1) + i + 1]));
                 }
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ks;
+                const float raw = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 // (also says that the other half has read its scores: P of this one lies where they were)
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                if (pair_any(pair, top > m + kLazy)) move_reference(top, j);
+                if (pair_any(pair, fmaf(raw, scale, shift) > kLazy)) move_reference(raw, j);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 uint32_t p[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     const int k = 2 * i & 31;
                     float x, y;
-                    scaled2(s[i >> 4][k], s[i >> 4][k + 1], ks, -m, x, y);
+                    scaled2(s[i >> 4][k], s[i >> 4][k + 1], scale, shift, x, y);
                     p[i] = pack2(ex2(x), ex2(y));
                 }
                 tmem_st32(ts + 32 * half, p);
@@ -507,7 +530,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             }
             const uint32_t sum = tmem_ld1(tq + cL);
             if (half == 0 && row < rows) {
-                part[(int64_t)sch.row_tile * 128 + row] = m * 0.6931471805599453f;  // the join works in natural-log units
+                part[(int64_t)sch.row_tile * 128 + row] = reference() * 0.6931471805599453f;  // the join works in natural-log units
                 part[(int64_t)sch.row_tile * 129 + row] = __uint_as_float(sum);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
