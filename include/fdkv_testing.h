@@ -22,6 +22,10 @@ extern "C" {
 fdkv_status fdkv_test_wait_expiry(fdkv_ctx* ctx, int32_t poll_cap, void* stream);
 fdkv_status fdkv_test_clear_device_status(fdkv_ctx* ctx, void* stream);
 
+/* The same for the wait of a warp for a counter in shared memory; the limit that the library's kernels give it, in polls.  */
+fdkv_status fdkv_test_count_expiry(fdkv_ctx* ctx, int32_t poll_cap, void* stream);
+int32_t fdkv_test_count_cap(void);
+
 /*
  * Which form the probe of a bf16 / head_dim 128 context with the entry rule takes for the keys that every query sees: 0 the
  * library's rule, 1 second moments, 2 products.  Per context, until changed.

@@ -75,6 +75,7 @@ def _load():
         "fdkv_device_status": [vp],
         "fdkv_compress_unit_noalloc": [vp, vp, i64, i32, i32, i32, i32, i32, vp, vp, vp, P(i32), vp],
         "fdkv_test_wait_expiry": [vp, i32, vp],
+        "fdkv_test_count_expiry": [vp, i32, vp],
         "fdkv_test_plan_shared": [i32] * 6 + [vp] + [i32] * 5 + [vp, vp],
         "fdkv_test_clear_device_status": [vp, vp],
     }
@@ -561,6 +562,10 @@ class Context:
     def test_wait_expiry(self, poll_cap: int, stream=None):
         """Runs a bounded device-side wait that nobody satisfies; device_status() then reports the timeout (7)."""
         _check(_lib.fdkv_test_wait_expiry(self.h, int(poll_cap), _stream(stream)), "fdkv_test_wait_expiry")
+
+    def test_count_expiry(self, poll_cap: int, stream=None):
+        """The same for the wait for a counter."""
+        _check(_lib.fdkv_test_count_expiry(self.h, int(poll_cap), _stream(stream)), "fdkv_test_count_expiry")
 
     def test_clear_device_status(self, stream=None):
         _check(_lib.fdkv_test_clear_device_status(self.h, _stream(stream)), "fdkv_test_clear_device_status")

@@ -35,4 +35,23 @@ __device__ __forceinline__ void mbar_wait_bounded(uint32_t bar, uint32_t parity,
     atomicMax(status, (int32_t)kFlagTimeout);
 }
 
+// Waits, a whole warp at a time, until a counter in shared memory has reached `target`.  One lane polls and sleeps in between: a plain load does not suspend the
+// warp as a barrier's wait does, so that without the sleep the polls would take issue slots from the warps at work, and their limit would be up in a tenth of a second.
+constexpr uint32_t kCountCap = 1u << 25;  // polls (seconds)
+__device__ __forceinline__ void count_wait_bounded(const volatile uint32_t* count, uint32_t target, volatile uint32_t* abort_flag, int32_t* status,
+                                                   uint32_t cap = kCountCap) {
+    if ((threadIdx.x & 31) == 0) {
+        uint32_t i = 0;
+        while (*count < target && !*abort_flag) {
+            if (i++ >= cap) {
+                *abort_flag = 1;
+                atomicMax(status, (int32_t)kFlagTimeout);
+                break;
+            }
+            __nanosleep(100);
+        }
+    }
+    __syncwarp();
+}
+
 }  // namespace fdkv

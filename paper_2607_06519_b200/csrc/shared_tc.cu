@@ -289,9 +289,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             }
             // A phase of the ring can be told from the one before, not from the one before that.  Within a run every fourth slot is this
             // warp's; runs without entries it passes at once, so that it waits until the producer, which has waited for slots all along, is here.
-            for (uint32_t i = 0; *run_no < runs && !*abort_flag; ++i)
-                if (i >= kWaitCap) { *abort_flag = 1; atomicMax(a.status, (int32_t)kFlagTimeout); }
-            __syncwarp();
+            count_wait_bounded(run_no, runs, abort_flag, a.status);
             const int slices = (ud.T + kResTile - 1) / kResTile;
             const uint32_t flip = ud.sign < 0.f ? 0x8000u : 0u;
             const bool tokens = ud.res_kind == 1, packed = !tokens && !ud.k_val, twice = ud.sign == 2.f && !a.twice;

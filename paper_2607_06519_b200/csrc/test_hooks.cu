@@ -29,10 +29,29 @@ __global__ void __launch_bounds__(32) wait_expiry_kernel(int32_t* status, uint32
     __syncthreads();
 }
 
+// The same for the wait for a counter that nobody advances.
+__global__ void __launch_bounds__(32) count_expiry_kernel(int32_t* status, uint32_t cap) {
+    __shared__ uint32_t abort_flag, count;
+    if (threadIdx.x == 0) abort_flag = count = 0;
+    __syncthreads();
+    count_wait_bounded(&count, 1u, &abort_flag, status, cap);
+    count_wait_bounded(&count, 1u, &abort_flag, status, cap);  // returns at once: the abort flag is up
+}
+
 }  // namespace
 }  // namespace fdkv
 
 extern "C" {
+
+int32_t fdkv_test_count_cap(void) { return (int32_t)fdkv::kCountCap; }
+
+fdkv_status fdkv_test_count_expiry(fdkv_ctx* c, int32_t poll_cap, void* stream) {
+    if (!c || poll_cap < 1 || poll_cap > 65536) return FDKV_ERR_INVALID_ARG;
+    fdkv::count_expiry_kernel<<<1, 32, 0, reinterpret_cast<cudaStream_t>(stream)>>>(reinterpret_cast<int32_t*>(c->work + c->ws.status), (uint32_t)poll_cap);
+    fdkv::count_launch(1);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? FDKV_OK : fdkv::record_cuda_error(e);
+}
 
 fdkv_status fdkv_test_wait_expiry(fdkv_ctx* c, int32_t poll_cap, void* stream) {
     if (!c || poll_cap < 1 || poll_cap > 65536) return FDKV_ERR_INVALID_ARG;
