@@ -205,29 +205,36 @@ class Rotary:
         m = len(inv_freq)
         if axis_of is not None and len(axis_of) != m:
             raise ValueError("axis_of needs one entry per frequency")
-        for w in (q_weight, k_weight):
-            if w is not None and (w.dim() != 1 or w.stride(0) != 1):
-                raise ValueError("norm weights must be dense [head_dim] tensors")
         self._inv = (C.c_float * max(m, 1))(*[float(f) for f in inv_freq])
         self._axis = None if axis_of is None else (C.c_int32 * max(m, 1))(*[int(a) for a in axis_of])
         self.n_axes, self.q_weight, self.k_weight = n_axes, q_weight, k_weight
-        devices = {w.get_device() for w in (q_weight, k_weight) if w is not None}
-        if len(devices) > 1:
+        self._rest = (2 * m, int(interleaved), n_axes, eps, scale, C.addressof(self._inv), None if self._axis is None else C.addressof(self._axis))
+        self._c = {}  # sizes -> (what the weights are, struct): one for each (a call reads it while other threads may make calls of other sizes)
+        for w in (q_weight, k_weight):
+            if w is not None and (w.dim() != 1 or w.stride(0) != 1):
+                raise ValueError("norm weights must be dense [head_dim] tensors")
+        if q_weight is not None and k_weight is not None and q_weight.get_device() != k_weight.get_device():
             raise ValueError("norm weights must be on one device")
-        self.device = devices.pop() if devices else None
-        self._rest = (2 * m, int(interleaved), n_axes, eps, scale, C.addressof(self._inv), None if self._axis is None else C.addressof(self._axis),
-                      None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
-        self._c = {}  # one struct for each set of sizes (a call reads it while other threads may make calls of other sizes)
+
+    @property
+    def device(self):
+        """The weights' device (None without weights)."""
+        w = self.k_weight if self.q_weight is None else self.q_weight
+        return None if w is None else w.get_device()
 
     def c(self, n_q_heads: int, n_kv_heads: int, head_dim: int, tdtype) -> _Rotary:
-        rows = (n_q_heads, n_kv_heads, head_dim, tdtype)
-        r = self._c.get(rows)
-        if r is None:
-            for w in (self.q_weight, self.k_weight):
-                if w is not None and (w.dtype is not tdtype or len(w) != head_dim):
-                    raise ValueError("norm weights must have the rows' dtype and head_dim")
-            r = self._c[rows] = _Rotary(n_q_heads, n_kv_heads, head_dim, _dtype_code(tdtype), *self._rest)
-        return r
+        rows, q, k = (n_q_heads, n_kv_heads, head_dim, tdtype), self.q_weight, self.k_weight
+        # (as they are now: a module may have given its parameters new memory)
+        weights = (None if q is None else (q.data_ptr(), q.dtype, q.shape, q.stride()), None if k is None else (k.data_ptr(), k.dtype, k.shape, k.stride()))
+        kept = self._c.get(rows)
+        if kept is None or kept[0] != weights:
+            for w in weights:
+                if w is not None and w[1:] != (tdtype, (head_dim,), (1,)):
+                    raise ValueError("norm weights must be dense [head_dim] tensors of the rows' dtype")
+            if q is not None and k is not None and q.get_device() != k.get_device():
+                raise ValueError("norm weights must be on one device")
+            kept = self._c[rows] = (weights, _Rotary(*rows[:3], _dtype_code(tdtype), *self._rest, *[w and w[0] for w in weights]))
+        return kept[1]
 
 
 def _dtype_code(tdtype) -> int:

@@ -1,0 +1,28 @@
+"""A Rotary goes with its weights where their module puts them (type, device or memory of its parameters); no device is needed."""
+import pytest
+import torch
+
+from paper_2607_06519_b200 import binding as B
+
+
+def test_weights_that_move():
+    w = torch.nn.Parameter(torch.ones(128, dtype=torch.bfloat16))
+    r = B.Rotary([1.0] * 64, q_weight=w)
+    first = r.c(4, 2, 128, torch.bfloat16)
+    assert (first.q_weight, first.k_weight) == (w.data_ptr(), None)
+    assert r.c(4, 2, 128, torch.bfloat16) is first
+    other = w.data.clone()
+    w.data = other  # (what Module.to and Module._apply do)
+    again = r.c(4, 2, 128, torch.bfloat16)
+    assert again.q_weight == other.data_ptr() != first.q_weight
+    w.data = w.data.float()
+    with pytest.raises(ValueError):
+        r.c(4, 2, 128, torch.bfloat16)
+    assert r.c(4, 2, 128, torch.float32).q_weight == w.data_ptr()
+    w.data = torch.ones(256)[::2]
+    with pytest.raises(ValueError):
+        r.c(4, 2, 128, torch.float32)
+    w.data = torch.ones(64)
+    with pytest.raises(ValueError):
+        r.c(4, 2, 128, torch.float32)
+    assert r.c(4, 2, 64, torch.float32).q_weight == w.data_ptr()
