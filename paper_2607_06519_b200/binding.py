@@ -259,6 +259,8 @@ def qk_norm_rope(rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream
     x = q if q is not None else k
     if x is None:
         raise ValueError("queries or keys are needed")
+    if (q is None and q_out is not None) or (k is None and k_out is not None):
+        raise ValueError("an output needs its input")
     n, _, d = x.shape
     dtype, device = x.dtype, x.get_device()
     qp = kp = qop = kop = None

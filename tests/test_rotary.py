@@ -1,4 +1,4 @@
-"""A Rotary goes with its weights where their module puts them (type, device or memory of its parameters); no device is needed."""
+"""What a Rotary and qk_norm_rope check before a call: weights whose module moved them, outputs without inputs; no device is needed."""
 import pytest
 import torch
 
@@ -26,3 +26,10 @@ def test_weights_that_move():
     with pytest.raises(ValueError):
         r.c(4, 2, 128, torch.float32)
     assert r.c(4, 2, 64, torch.float32).q_weight == w.data_ptr()
+
+
+def test_an_output_without_its_input_is_refused():
+    r, x, pos = B.Rotary([1.0] * 32), torch.zeros((3, 2, 64)), torch.zeros(3, dtype=torch.int32)
+    for kw in (dict(q=x, k=None, k_out=x.clone()), dict(q=None, k=x, q_out=x.clone())):
+        with pytest.raises(ValueError, match="needs its input"):
+            B.qk_norm_rope(r, positions=pos, **kw)
