@@ -237,8 +237,10 @@ fdkv_status fdkv_decode_step_host(fdkv_ctx* ctx, int32_t batch, const void* q /*
  * seqs: HOST int32[batch], distinct slots, batch <= 1024; each is prompt_seq itself (which then goes on with its own tail) or a
  * slot without a committed prompt (FDKV_ERR_STATE).  A sequence may have no tail rows at all.  The prompt is what the slot holds
  * committed at the time of the call: after fdkv_fold_tail on it, the folded tokens belong to it for every sequence.
- * bf16 storage with head_dim 128: the prompt's probabilities are rounded to bf16 for the second product (float32 sums), so that out is
- * within about 1e-3 of the exact attention before its own rounding; the rest in float32 (1e-6).  FDKV_ROWS_E4M3 contexts: FDKV_ERR_UNSUPPORTED.
+ * bf16 storage with head_dim 128: for bf16 outputs the prompt's probabilities p_t are rounded to bf16 for the second product (float32 sums), so
+ * that out is within 2^-8 sum_t p_t |v_t| of the exact attention before its own rounding, as a rule within a quarter of that; fdkv_decode_attn's have 16
+ * bits.  For float32 outputs this call's have 16 as well (2^-16 in place of 2^-8), which takes 4 to 30 % longer.  Other contexts compute in
+ * float32.  FDKV_ROWS_E4M3 contexts: FDKV_ERR_UNSUPPORTED.
  * A query whose logits are all minus infinity gets zeros.
  * Like fdkv_decode_attn's, a call's split-K parts lie in the workspace: calls of one context on several streams, replays of
  * captured ones among them, are ordered by the caller.

@@ -16,6 +16,9 @@
 // of ones: what is wrong with a probability then shifts the mean instead of scaling it (a row with one large probability is not
 // off at all), and the softmax has no additions to do.  (Sums of the unrounded ones: outputs off by 2.3e-3 instead of 1.7e-3, of which 1.7e-3 is the
 // rounding of the outputs.)
+// For float32 outputs, whose rounding does not hide it, what bf16 leaves of P goes through the same products: P of 16 bits, 24 products a tile more with
+// entries, 16 without (us a call with bf16 and with float32 outputs: 8 191 tokens, 16 sequences 19.3 and 21.1; 32 768 tokens, 8 sequences 31.9 and 38.7, 64
+// sequences 58.9 and 74.7; 131 072 tokens, 16 sequences 95.2 and 123.5).
 //
 // What bounds it.  One row group (a batch of up to 128 query rows per KV head): memory, as long as few heads are residual.  32 768 tokens, 8 KV heads x 4, 8 sequences, a
 // sixteenth kept in three heads: 141 MB, 22 us of the call's 31 with nothing in L2, the rest its start, first copies and the join (131 072
@@ -141,6 +144,8 @@ __device__ __forceinline__ bool next_run(const SharedSched& sch, int& g, int g_e
 }
 
 // 640 threads x 96 registers at launch; the softmax's two warpgroups take 112, the others keep 80 (together 464 of the 480 per thread of a warpgroup; 72 spilled, which cost 3 %).
+// FINE: what bf16 leaves of P takes the score columns that P does not, and both products with P once more (see above).
+template <bool FINE>
 __global__ void __launch_bounds__(kThreads, 1)
 shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const __grid_constant__ SharedSched sch) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -225,6 +230,7 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
             // the loop behind `if (lane == 0)` issuing a tile's products took 2 700 cycles, more than the softmax.
             const bool leader = elect_one();
             const uint64_t one = smem_desc(ones);
+            constexpr int kParts = FINE ? 16 : 8;  // slices of 16 tokens of P, then of what is left of it
             int it = 0;
             uint32_t qph = 0;
             bool ok = true;
@@ -260,10 +266,10 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                         const uint32_t tp = tmem + cS + (it & 1) * 128;
                         if (leader && ok) {
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) umma_ts<kIdescO>(tmem + cO, tp + 8 * k, d + k * (2048 >> 4), j > 0 || e > 0 || k > 0);
+                            for (int k = 0; k < kParts; ++k) umma_ts<kIdescO>(tmem + cO, tp + 8 * k, d + (k & 7) * (2048 >> 4), j > 0 || e > 0 || k > 0);
                             if (e == 0)
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) umma_ts<kIdescL>(tmem + cL, tp + 8 * k, one, j > 0 || k > 0);
+                                for (int k = 0; k < kParts; ++k) umma_ts<kIdescL>(tmem + cL, tp + 8 * k, one, j > 0 || k > 0);
                             umma_commit(sm0 + oEmpty + 8 * sl);
                             if (e + 1 == parts) umma_commit(sm0 + oO + 8 * (it & 1));
                         }
@@ -496,15 +502,33 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 if (pair_any(pair, fmaf(raw, scale, shift) > kLazy)) move_reference(raw, j);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                uint32_t p[32];
+                if constexpr (FINE) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int k = 2 * i & 31;
-                    float x, y;
-                    scaled2(s[i >> 4][k], s[i >> 4][k + 1], scale, shift, x, y);
-                    p[i] = pack2(ex2(x), ex2(y));
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t p[16], rest[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float x, y;
+                            scaled2(s[c][2 * i], s[c][2 * i + 1], scale, shift, x, y);
+                            x = ex2(x);
+                            y = ex2(y);
+                            p[i] = pack2(x, y);
+                            rest[i] = pack2(x - __uint_as_float(p[i] << 16), y - __uint_as_float(p[i] & 0xFFFF0000u));
+                        }
+                        tmem_st16(ts + 32 * half + 16 * c, p);
+                        tmem_st16(ts + 64 + 32 * half + 16 * c, rest);
+                    }
+                } else {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int k = 2 * i & 31;
+                        float x, y;
+                        scaled2(s[i >> 4][k], s[i >> 4][k + 1], scale, shift, x, y);
+                        p[i] = pack2(ex2(x), ex2(y));
+                    }
+                    tmem_st32(ts + 32 * half, p);
                 }
-                tmem_st32(ts + 32 * half, p);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
@@ -547,7 +571,10 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tmap, SharedArgs a, const _
 
 cudaError_t launch_shared_tc(const SharedArgs& a, const SharedSched& sch, cudaStream_t st) {
     static PerDevice once;
-    const cudaError_t e = once.ensure([]() { return cudaFuncSetAttribute(shared_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
+    const cudaError_t e = once.ensure([]() {
+        const cudaError_t e = cudaFuncSetAttribute(shared_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(shared_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(sch.ranges * sch.groups);
@@ -559,7 +586,7 @@ cudaError_t launch_shared_tc(const SharedArgs& a, const SharedSched& sch, cudaSt
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, shared_tc_kernel, *reinterpret_cast<const CUtensorMap*>(a.tmap), a, sch);
+    return cudaLaunchKernelEx(&cfg, a.out_dtype == FDKV_F32 ? shared_tc_kernel<true> : shared_tc_kernel<false>, *reinterpret_cast<const CUtensorMap*>(a.tmap), a, sch);
 }
 
 }  // namespace fdkv
