@@ -121,9 +121,17 @@ typedef enum { FDKV_RESIDUAL_ENTRIES = 0, FDKV_RESIDUAL_TOKENS = 1 } fdkv_residu
 
 typedef struct fdkv_ctx fdkv_ctx;
 
-/* Bytes the caller must provide.  arena_bytes is the worst case (every unit in exact mode). */
+/* Bytes the caller must provide.  arena_bytes is the worst case (every slot committed, every unit in exact mode). */
 fdkv_status fdkv_sizes(const fdkv_config* cfg /*HOST*/, size_t* arena_bytes /*HOST*/,
                        size_t* workspace_bytes /*HOST*/);
+
+/*
+ * The same where at most n_prompts (1 .. max_batch) of the slots hold a committed prompt at a time, each of up to max_prefill tokens in
+ * any modes: 1 for a batch on one shared prompt (fdkv_decode_attn_shared), whose other slots have tails only.  fdkv_create takes every arena that
+ * has room for the tails; fdkv_commit returns FDKV_ERR_ARENA_FULL for a prompt that no longer fits.
+ */
+fdkv_status fdkv_sizes_prompts(const fdkv_config* cfg /*HOST*/, int32_t n_prompts, size_t* arena_bytes /*HOST*/,
+                               size_t* workspace_bytes /*HOST*/);
 
 /* Creates the host-side context over caller-owned device memory and zero-initialises the tail counters
  * and the device status word (synchronously, on the legacy default stream).  The context keeps the pointers;

@@ -48,6 +48,7 @@ def _load():
     P = C.POINTER
     sig = {
         "fdkv_sizes": [P(_Config), P(sz), P(sz)],
+        "fdkv_sizes_prompts": [P(_Config), i32, P(sz), P(sz)],
         "fdkv_create": [P(_Config), vp, sz, vp, sz, P(vp)],
         "fdkv_reset": [vp],
         "fdkv_compress_prefill": [vp, i32, i32, i32, i32, P(vp), P(vp), i64, i64, vp],
@@ -137,9 +138,13 @@ class Config:
         return _Config(*(int(getattr(self, f[0])) for f in _Config._fields_))
 
 
-def sizes(cfg: Config):
+def sizes(cfg: Config, prompts: int | None = None):
+    """(arena, workspace) bytes; prompts: slots that hold a committed prompt at a time (None: all)."""
     a, w = C.c_size_t(0), C.c_size_t(0)
-    st = _lib.fdkv_sizes(C.byref(cfg.c()), C.byref(a), C.byref(w))
+    if prompts is None:
+        st = _lib.fdkv_sizes(C.byref(cfg.c()), C.byref(a), C.byref(w))
+    else:
+        st = _lib.fdkv_sizes_prompts(C.byref(cfg.c()), prompts, C.byref(a), C.byref(w))
     if st:
         raise FdkvError(st, "fdkv_sizes")
     return a.value, w.value
@@ -331,15 +336,16 @@ def _slots(seqs):
 
 
 class Context:
-    """One fdkv context over torch-owned device memory."""
+    """One fdkv context over torch-owned device memory; prompts: slots that hold a committed prompt at a time (None: all), which sizes the arena
+    unless arena_bytes does."""
 
-    def __init__(self, cfg: Config, device="cuda:0", arena_bytes: int | None = None):
+    def __init__(self, cfg: Config, device="cuda:0", arena_bytes: int | None = None, prompts: int | None = None):
         if not torch.cuda.is_available():
             raise RuntimeError("fdkv needs a CUDA device; there is no CPU path")
         self.cfg = cfg
         self.device = torch.device(device)
         self.tdtype = torch.bfloat16 if cfg.dtype == BF16 else torch.float32
-        worst, work = sizes(cfg)
+        worst, work = sizes(cfg, prompts)
         self.arena_bytes = int(arena_bytes if arena_bytes is not None else worst)
         with torch.cuda.device(self.device):
             self.arena = torch.empty(self.arena_bytes, dtype=torch.uint8, device=self.device)

@@ -130,7 +130,7 @@ void make_layouts(const Shape& s, WsLayout& w, ArenaLayout& a) {
                                   : 2 * rows_pad + 2 * (size_t)s.NB * (align_up((size_t)(s.kcap + s.kfold_max) * 4) + align_up((size_t)(s.kcap + s.kfold_max) * s.esize)) +
                                         2 * align_up((size_t)(s.kcap + s.kfold_max) * 4) +
                                         2 * align_up((size_t)(s.ntiles_max + s.max_fold / kResTile + 2) * 4);
-    a.worst_total = a.bump + (size_t)s.max_batch * s.NU * (exact_unit > resid_unit ? exact_unit : resid_unit);
+    a.prompt = (size_t)s.NU * (exact_unit > resid_unit ? exact_unit : resid_unit);
 }
 
 inline cudaStream_t S(void* p) { return reinterpret_cast<cudaStream_t>(p); }
@@ -279,15 +279,20 @@ cudaError_t launch_set_tail_len(int32_t* tail_len, int L, int max_batch, int seq
 
 extern "C" {
 
-fdkv_status fdkv_sizes(const fdkv_config* cfg, size_t* arena_bytes, size_t* workspace_bytes) {
+fdkv_status fdkv_sizes_prompts(const fdkv_config* cfg, int32_t n_prompts, size_t* arena_bytes, size_t* workspace_bytes) {
     Shape s;
     if (!cfg || !make_shape(*cfg, s)) return cfg ? FDKV_ERR_UNSUPPORTED : FDKV_ERR_INVALID_ARG;
+    if (n_prompts < 1 || n_prompts > s.max_batch) return FDKV_ERR_INVALID_ARG;
     WsLayout w;
     ArenaLayout a;
     make_layouts(s, w, a);
-    if (arena_bytes) *arena_bytes = a.worst_total;
+    if (arena_bytes) *arena_bytes = a.bump + (size_t)n_prompts * a.prompt;
     if (workspace_bytes) *workspace_bytes = w.total;
     return FDKV_OK;
+}
+
+fdkv_status fdkv_sizes(const fdkv_config* cfg, size_t* arena_bytes, size_t* workspace_bytes) {
+    return fdkv_sizes_prompts(cfg, cfg ? cfg->max_batch : 0, arena_bytes, workspace_bytes);
 }
 
 fdkv_status fdkv_create(const fdkv_config* cfg, void* arena, size_t arena_bytes, void* workspace,

@@ -108,7 +108,7 @@ struct WsLayout {
         partials, io_q, io_k, io_v, io_out, jobs, total;  // io_*: host-I/O staging, [L] layers each
 };
 struct ArenaLayout {
-    size_t tail_len, desc, tail_k, tail_v, bump, worst_total;
+    size_t tail_len, desc, tail_k, tail_v, bump, prompt;  // prompt: bytes of a committed one, at most
 };
 
 struct SeqState {
