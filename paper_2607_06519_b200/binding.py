@@ -345,7 +345,7 @@ class Context:
         self.cfg = cfg
         self.device = torch.device(device)
         self.tdtype = torch.bfloat16 if cfg.dtype == BF16 else torch.float32
-        worst, work = sizes(cfg, prompts)
+        worst, work = sizes(cfg) if prompts is None else sizes(cfg, prompts)
         self.arena_bytes = int(arena_bytes if arena_bytes is not None else worst)
         with torch.cuda.device(self.device):
             self.arena = torch.empty(self.arena_bytes, dtype=torch.uint8, device=self.device)
