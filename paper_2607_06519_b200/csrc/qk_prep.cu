@@ -4,14 +4,18 @@
 //   y = x / sqrt(mean_c x_c^2 + eps) * w          (no weights: y = x)
 //   (a, b) -> (a cos - b sin, b cos + a sin) * s  angle = pos[axis of the frequency] * inv_freq
 // All in float32 behind the storage type, one rounding at the end; the angle is a float64 product, whose whole turns are dropped
-// before it becomes a float32 (a float32 product of a position of 10^6 would be off by 0.06 rad).
+// before it becomes a float32 (a float32 product of a position of 10^6 would be off by 0.06 rad).  What is left, up to half a turn, is rounded to float32 once: with
+// float32 rows the outputs are off by 5.5e-8 (root mean square, relative), with float64 sines they would be by 4.2e-8; bf16 rows hide it.
 //
 // Bound by memory traffic for prompts, by the chain load -> norm -> store for a few tokens.  D / 8 lanes share a (token, head) row:
 // a lane holds four channels of the first half of the rotating ones and the four that pair with them, so that a warp's loads
 // cover whole 128-byte stretches, a norm costs log2(D / 8) shuffles and a rotation none.  The lanes that hold the same channels
 // of different rows share the token's sines: each computes its part of the four and hands them on by shuffle.
 // Measured: 32 768 tokens of 32 + 8 heads of 128 channels, out of and into strided rows, norm and rotation: 112 us for 671 MB, 6.0 TB/s; 16 383 tokens without
-// norms 57 us, 5.9 TB/s; one token 2.5 us.  (71 registers, 26 one-warp blocks on an SM.)
+// norms 57 us, 5.9 TB/s; one token 2.5 us.  (71 or 72 registers, 26 one-warp blocks on an SM.)  Float32 with norms spills 52 bytes, 80 with neighbouring pairs; 16 384
+// tokens of 32 + 8 heads of 128 channels take 111 us, without norms (and spills) 106, where the bytes need 102.7.
+// A warp works on one token and a group of rows is of one tensor, so that with few heads most lanes have no row and the sines are the work: 16 384 bf16 tokens
+// of 4 + 1 heads of 128 channels take 24 us without norms, of 1 + 1 heads 22.5, of 1 + 1 heads of 64 channels 18, where the bytes need 6.4, 2.6 and 1.3.
 // (Eight channels a lane, in 16-byte loads, needed 118 registers with weights: 16 warps on an SM, two groups of rows in flight each, 3.9 TB/s for
 // 32 768 tokens of 40 heads.)
 #include <cmath>

@@ -49,8 +49,10 @@ constexpr int part_smem() { return (kRows * (D + 4) + 2 * kTok * (D + 4) + kRows
 // the unit's scale is applied to the logits and the outputs) and multiplied with the group's query rows: a thread has two rows x
 // two tokens of the logits and 2 x D / 16 of the outputs.  float32 FMA; for float32 storage eight channels' products at a time
 // are added up in float64, since the exponential magnifies the rounding of logits of a few tens.
-// Bound by latency where it is used: the correctness workload's 4 099 tokens, 2 KV heads, 6 sequences make two tiles for each of 148 blocks, and a call of
-// 13.9 us is two dependent kernels, of which the bytes need 0.7.
+// Short prompts are bound by latency: the correctness workload's 4 099 tokens, 2 KV heads, 6 sequences make two tiles for each of 148 blocks, and a call of
+// 13.9 us is two dependent kernels, of which the bytes need 0.7.  From some thousand tokens on the loads from shared memory bound it, one of 16 bytes for every four products of
+// a thread: 8 to 10 TFLOP/s whatever the type.  8 KV heads x 4, 8 and 64 sequences, us (and what the bytes need): float32 of 128 channels, 8 192 tokens 116 and 898 (10.6),
+// 32 768 tokens 445 and 3 541 (42.5); of 64 channels 71 and 539 (5.3), 268 and 2 105 (21.3); bf16 of 64 channels 89 and 500 (2.7), 349 and 2 075 (10.7).
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) shared_part_kernel(SharedArgs a, const __grid_constant__ SharedSched sch) {
     using ACC = typename std::conditional<sizeof(T) == 4, double, float>::type;
@@ -323,7 +325,8 @@ constexpr int kJoinWarps = 8;
 
 // Portable join.  grid (Hkv, batch).  D / 8 lanes share a tail token, eight channels each; every such lane group keeps a softmax state of its own,
 // joined through shared memory with the prompt's parts.  The tails, q and the new rows are read before the dependency wait: the
-// prompt kernel lets this one start only behind its own, when all they come from is complete.  Bound by the chain of its loads.
+// prompt kernel lets this one start only behind its own, when all they come from is complete.  Bound by the chain of its loads.  (Eight float32 heads a group need more than
+// 255 registers: 280 bytes spilled.)
 template <typename T, int D, int G, int NB>
 __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(SharedArgs a, const __grid_constant__ SharedSched sch, const __grid_constant__ SharedSeqs<NB> sq) {
     using ACC = typename std::conditional<sizeof(T) == 4, double, float>::type;
@@ -499,7 +502,8 @@ __device__ __forceinline__ float peer_load(uint32_t addr) {
 // product for it, so that P acts with 16 bits.  Blocks of a cluster share a unit's tail and parts (small batches, long tails).
 // Bound by memory and the loads on their way: 64 sequences of 200 tokens are 52 MB of tails, 10 us of a call (8 at the copy rate), of 1 000 262 MB, 50 us; for small
 // batches by the chain parts -> sums -> outputs behind the prompt kernel, with ten parts on their way at a time.
-// BLOCKS: on an SM at least.  Three keep all of a warp's registers; four, for more blocks than three have room for, keep more tail rows on their way
+// A prompt block fills its SM, so that where there is one on every SM no block of this kernel runs before a prompt block has left: the tails' bytes come behind the prompt's.
+// BLOCKS: on an SM at least.  Three keep all of a warp's registers; four (128 registers, 28 to 44 bytes spilled), for more blocks than three have room for, keep more tail rows on their way
 // (32 768 and 2 048 tokens, 64 sequences of 200 tail tokens: 67.1 -> 64.8 and 27.3 -> 22.8 us; 32 sequences, which three hold, 17.3 and 19.7).
 template <int G, int NB, int BLOCKS>
 __global__ void __launch_bounds__(kTcWarps * 32, BLOCKS) shared_join_tc_kernel(SharedArgs a, const __grid_constant__ SharedSched sch, const __grid_constant__ SharedSeqs<NB> sq) {
@@ -555,7 +559,7 @@ __global__ void __launch_bounds__(kTcWarps * 32, BLOCKS) shared_join_tc_kernel(S
                 v[i][1] = __ldcg(reinterpret_cast<const uint4*>(p + 64));
             }
             // The next step's rows, one a lane, on their way to L2 (64 sequences of 1 000 own tokens: 82.9 -> 62.0 us; two steps ahead 67.5, both
-            // 69.8; of 200, 22.6 -> 23.5 behind 2 048 tokens and 64.6 -> 62.4 behind 32 768).
+            // 69.8; of 200, 22.6 -> 23.5 behind 2 048 tokens and 64.6 -> 62.4 behind 32 768: asked for in either case, since the tail's length does not tell these apart).
             if (t0 + step < n) {
                 const int t = t0 + step + (lane & 15);
                 if (t < n) {

@@ -24,8 +24,10 @@
 // sixteenth kept in three heads: 141 MB, 22 us of the call's 31 with nothing in L2, the rest its start, first copies and the join (131 072
 // tokens: 96 us for 556 MB, 5.8 TB/s).  A tile with entries needs 32 + 8 products instead of 16 + 8, 3 460 cycles of the tensor pipe, twice what its
 // rows need from memory; ranges are cut by cost, so that blocks without such tiles do more of the rest.
-// Two groups (64 sequences): the softmax, 1 500 + 250 cycles a tile (its 16 384 exponentials take 1 024), and the tensor pipe at 55 %;
-// 42 us for the two groups' 4 096 tiles.
+// What a tile takes a block, from the difference of 65 536 and 32 768 tokens with all heads in one mode: one row group 1.37 us without entries (7.1 TB/s of reads), 1.78
+// with them (3 500 cycles); two row groups (64 sequences) 1.20 and 1.92 us.  With two groups the rows come once from memory for both, at a third of its rate, the tensor pipe is
+// busy for 54 % of the time, and the exponentials (16 384 a tile) take 1 024 of the 2 350 cycles of a tile without entries: no one unit bounds it, and what makes up the
+// rest of those cycles has not been measured.  32 768 tokens, three of eight heads with entries: 27.7 tiles a block, 41 us.
 #include <cuda.h>
 
 #include "fdkv_internal.h"
