@@ -14,7 +14,7 @@ extern "C" {
 
 /*
  * Launches one thread block whose thread 0 waits, with the library's bounded mbarrier wait, on a barrier that nobody
- * ever arrives at, with a limit of `poll_cap` polls (1 .. 65536; a thousand polls take microseconds).  The wait runs
+ * ever arrives at, with a limit of `poll_cap` polls (1 .. 65536; a thousand polls take a tenth of a millisecond).  The wait runs
  * out, raises the block's abort flag and the context's device status word and the kernel returns normally: afterwards
  * fdkv_device_status(ctx) reports FDKV_ERR_TIMEOUT, exactly as after a copy that never landed in a decode or probe
  * kernel.  Nothing faults and nothing hangs; the context stays usable.  fdkv_test_clear_device_status resets the word.

@@ -10,7 +10,7 @@
 
 namespace fdkv {
 
-constexpr uint32_t kWaitCap = 1u << 22;  // polls before a wait gives up (seconds, where a copy lands within microseconds)
+constexpr uint32_t kWaitCap = 1u << 22;  // polls before a wait gives up (0.4 s at 100 ns each, where a copy lands within microseconds)
 
 __device__ __forceinline__ uint32_t mbar_try_wait(uint32_t bar, uint32_t parity) {
     uint32_t ok;
@@ -37,7 +37,7 @@ __device__ __forceinline__ void mbar_wait_bounded(uint32_t bar, uint32_t parity,
 
 // Waits, a whole warp at a time, until a counter in shared memory has reached `target`.  One lane polls and sleeps in between: a plain load does not suspend the
 // warp as a barrier's wait does, so that without the sleep the polls would take issue slots from the warps at work, and their limit would be up in a tenth of a second.
-constexpr uint32_t kCountCap = 1u << 25;  // polls (seconds)
+constexpr uint32_t kCountCap = 1u << 25;  // polls (8 s at 256 ns each: it may have to wait for a block's whole heads)
 __device__ __forceinline__ void count_wait_bounded(const volatile uint32_t* count, uint32_t target, volatile uint32_t* abort_flag, int32_t* status,
                                                    uint32_t cap = kCountCap) {
     if ((threadIdx.x & 31) == 0) {
